@@ -83,7 +83,8 @@ enum { KATA_LAYOUT_DIRECT = 0, KATA_LAYOUT_PACKED = 1 }; /* kata_opts.state_layo
 enum { KATA_SEQUENTIAL = 0, KATA_SCAN = 1, KATA_INTER_AUTO = 2 };   /* kata_opts.inter_chunk */
 enum { KATA_IMPL_AUTO = 0, KATA_IMPL_SIMT = 1, KATA_IMPL_TENSOR = 2 }; /* kata_opts.impl */
 enum { KATA_FN_QUADRATIC = 0, KATA_FN_CHUNKED = 1, KATA_FN_CHUNK_STATE_SCAN = 2, KATA_FN_DECODE_STEP = 3,
-       KATA_FN_BWD_QUADRATIC = 4, KATA_FN_BWD_CHUNKED = 5 };
+       KATA_FN_BWD_QUADRATIC = 4, KATA_FN_BWD_CHUNKED = 5, KATA_FN_SSM_SCAN = 6, KATA_FN_BWD_NORM_ROPE = 7,
+       KATA_FN_BWD_SHORT_CONV = 8 };
 
 /*
  * Options (plain data; zero-initialise, then set struct_size = sizeof(kata_opts)).
@@ -315,6 +316,119 @@ int kata_fwd_host(int fn, const void* q_host, const void* k_host, const void* v_
 #define KATA_STATIC_SCRATCH_BYTES (32u << 20)
 int kata_chunk_state_scan_static(const void* q, const void* k, const void* v, void* out,
                                  int B, int H, int T, int d_k, int d_v, int C, const kata_opts* opts);
+
+/*
+ * ---- Around the attention: rows before it, and the decayed recurrence beside it ----
+ *
+ * The operators below take their tensors as views: sizes in the argument struct (zero-initialise, then set struct_size), a
+ * pointer and the strides, in elements, of all axes but the innermost, whose entries lie side by side.  So the rows of a packed
+ * projection or of the convolution's output are read where they are.  Of kata_opts they read dtype, impl, workspace,
+ * device_status and stream; the state pointers in it must be null, the rest is ignored.  Conventions as above: the caller owns
+ * every buffer, nothing is allocated, nothing synchronises, the calls can be captured, all arithmetic is fp32 and a result is
+ * rounded once.  An output must not overlap an input (a state may be advanced in place); a stride of 0 is allowed for inputs.
+ * Sizes of 0 and negative strides are refused (KATA_ERR_INVALID_ARG).
+ *
+ * `lengths` (optional, device, [B] int32): the sequences of a padded batch end there (clamped to 0 .. T).  What lies behind a
+ * sequence's end is not read into any result, whatever it holds; output rows there are written as zeros.
+ */
+
+/*
+ * Norm of every query and key row by its root mean square and rotation by its token's position, in one pass (the rows that a
+ * layer gives to the attention; the "RoPE" of the section on positions):
+ *     y = R_p (w * x / sqrt(mean(x^2) + eps))
+ * R_p turns the pairs (i, i + rotary_dim / 2) (interleaved: (2i, 2i + 1)) of the first rotary_dim entries by p inv_freq[i]
+ * radians; the others are left.  The angle is formed as a fraction of a turn in 64-bit integers, exact to 2^-64 p turns, so far
+ * positions lose nothing.  Outputs are usually [B,H,T,d], what the attention takes.
+ *   d in {16, 32, 64, 128}; rotary_dim a multiple of 16 up to d (0: norm alone); rows 16-byte aligned (KATA_ERR_ALIGNMENT).
+ *   inv_freq: HOST array of rotary_dim / 2 values, read before the call returns.
+ *   positions: device int64, position of token (b, t) at b * pos_stride[0] + t * pos_stride[1]; null: pos_offset + t.
+ *   q_weight, k_weight: [d] in the element type, or null (ones).  H_k = 0: queries alone.
+ * kata_bwd_norm_rope: q_out and k_out hold the gradients of the outputs (read); writes dq, dk and, where the weights are set,
+ * dq_weight, dk_weight ([d] fp32, overwritten, summed over all rows in a fixed order; null: not wanted).
+ * Workspace: kata_workspace_bytes(KATA_FN_BWD_NORM_ROPE, B, H_q + H_k, T, d, 0, 0, opts) for the backward, none for the forward.
+ */
+typedef struct kata_norm_rope_args {
+  uint32_t struct_size;
+  int32_t B, T, H_q, H_k, d;
+  int32_t rotary_dim, interleaved;
+  double eps;
+  const double* inv_freq;
+  const int64_t* positions;
+  int64_t pos_stride[2];           /* batch, token */
+  int64_t pos_offset;
+  const void *q, *k;               /* strides: batch, head, token */
+  void *q_out, *k_out;
+  int64_t q_stride[3], k_stride[3], q_out_stride[3], k_out_stride[3];
+  const void *q_weight, *k_weight;
+  void *dq, *dk;                   /* backward only, from here on */
+  int64_t dq_stride[3], dk_stride[3];
+  float *dq_weight, *dk_weight;
+} kata_norm_rope_args;
+int kata_fwd_norm_rope(const kata_norm_rope_args* a, const kata_opts* opts);
+int kata_bwd_norm_rope(const kata_norm_rope_args* a, const kata_opts* opts);
+
+/*
+ * Short causal convolution of every channel along the tokens (what the paper's layers put before queries, keys and values):
+ *     y_t = act(bias + sum_{j < width} w[j] x_{t - width + 1 + j}),   act(z) = z, or z / (1 + e^-z) with silu
+ * x before the first token is zero, or s_init.  width in {2, 3, 4}, any number of channels D; weight [D][width] and bias [D]
+ * (or null) contiguous in the element type.
+ *   s_init, s_final: [B][D][width - 1] contiguous in the element type, the last width - 1 inputs, oldest first, before the first
+ *   token and after the last one of each sequence (either may be null; s_final may be s_init).
+ * kata_decode_short_conv: one token, T = 1 (t-strides ignored), s_init and s_final set.
+ * kata_bwd_short_conv: dout (read) takes the place of out; writes dx and, where set, dweight [D][width] and dbias [D] (fp32,
+ * overwritten, summed in a fixed order).  s_init and s_final must be null: the sequences start at their first token.
+ * Rows aligned to 16 bytes (pointers, strides and D) are read 16 bytes at a time, others entry by entry.
+ * Workspace: kata_workspace_bytes(KATA_FN_BWD_SHORT_CONV, B, D, T, width, 0, 0, opts) for the backward, else none.
+ */
+typedef struct kata_short_conv_args {
+  uint32_t struct_size;
+  int32_t B, T, D, width, silu;
+  const void *x, *weight, *bias;
+  void* out;
+  int64_t x_stride[2], out_stride[2];   /* batch, token */
+  const void* s_init;
+  void* s_final;
+  const int32_t* lengths;
+  const void* dout;                     /* backward only, from here on (out is not used) */
+  void* dx;
+  int64_t dout_stride[2], dx_stride[2];
+  float *dweight, *dbias;
+} kata_short_conv_args;
+int kata_fwd_short_conv(const kata_short_conv_args* a, const kata_opts* opts);
+int kata_decode_short_conv(const kata_short_conv_args* a, const kata_opts* opts);
+int kata_bwd_short_conv(const kata_short_conv_args* a, const kata_opts* opts);
+
+/*
+ * Selective state space scan: the first-order linear recurrence with a decay that every token sets, without the normaliser,
+ *     s_t = dt_t + dt_bias (dt_softplus: log(1 + e^that)),  a_t = exp(s_t A),
+ *     S_t = a_t S_{t-1} + s_t k_t v_t^T,   o_t = S_t^T q_t + D v_t
+ * per head, S in R^{n x d_v} in fp32 and in the layout of the first-order state of kata_decode_step.  Queries and keys are
+ * shared by the H / G heads of a group (head h reads group h / (H / G)).  n in {16, 32, 64, 128}, d_v in {16, 32, 64}, H a
+ * multiple of G, B * H <= 65535; q, k, v, out rows 16-byte aligned.  A, D, dt_bias: [H] fp32; D and dt_bias may be null (0).
+ * dt in the element type, any strides.  A <= 0 and s_t >= 0 are what the recurrence is for: a decay above 1 grows with the
+ * distance, and what overflows fp32 on the way is inf or NaN in the result.
+ *   s_init, s_final: [B,H,n,d_v] contiguous fp32, 16-byte aligned, the state before the first and after the last token of each
+ *   sequence (either may be null; s_final may be s_init).
+ * Forms: bf16 with n in {64, 128} and d_v = 64 on the tensor cores (chunks of 128 tokens: the weights inside a chunk and the
+ * state that it reads are rounded to bf16, the state that is carried is not); everything else token by token in fp32.  Few heads:
+ * the token axis is cut into segments, whose own states come first.
+ * Workspace: kata_workspace_bytes(KATA_FN_SSM_SCAN, B, H, T, n, d_v, 0, opts).
+ * kata_decode_ssm_step: one token of every head, T = 1 (t-strides ignored, lengths null), s_init = s_final = the state; no workspace.
+ */
+typedef struct kata_ssm_args {
+  uint32_t struct_size;
+  int32_t B, T, H, G, n, d_v;
+  int32_t dt_softplus;
+  const void *q, *k, *v, *dt;          /* strides: batch, head or group, token */
+  void* out;
+  int64_t q_stride[3], k_stride[3], v_stride[3], dt_stride[3], out_stride[3];
+  const float *A, *D, *dt_bias;
+  const float* s_init;
+  float* s_final;
+  const int32_t* lengths;
+} kata_ssm_args;
+int kata_fwd_ssm_scan(const kata_ssm_args* a, const kata_opts* opts);
+int kata_decode_ssm_step(const kata_ssm_args* a, const kata_opts* opts);
 
 /*
  * Bytes of device workspace entry point `fn` needs for these sizes and options (0 if none);

@@ -30,11 +30,14 @@ KATA_IMPL_AUTO, KATA_IMPL_SIMT, KATA_IMPL_TENSOR = 0, 1, 2
 KATA_FN_QUADRATIC, KATA_FN_CHUNKED, KATA_FN_CHUNK_STATE_SCAN, KATA_FN_DECODE_STEP = 0, 1, 2, 3
 KATA_FN_BWD_QUADRATIC = 4
 KATA_FN_BWD_CHUNKED = 5
+KATA_FN_SSM_SCAN, KATA_FN_BWD_NORM_ROPE, KATA_FN_BWD_SHORT_CONV = 6, 7, 8
 KATA_FN_HOST_IO = 0x100
 KATA_OK, KATA_ERR_INVALID_ARG, KATA_ERR_UNSUPPORTED_SHAPE, KATA_ERR_WORKSPACE_TOO_SMALL, KATA_ERR_DEVICE_TIMEOUT = 0, -1, -2, -4, -7
 
 EXPORTS = ("kata_fwd_quadratic", "kata_fwd_chunked", "kata_chunk_state_scan", "kata_chunk_state_scan_static",
            "kata_fwd_host", "kata_decode_step", "kata_bwd_quadratic", "kata_bwd_chunked",
+           "kata_fwd_norm_rope", "kata_bwd_norm_rope", "kata_fwd_short_conv", "kata_decode_short_conv", "kata_bwd_short_conv",
+           "kata_fwd_ssm_scan", "kata_decode_ssm_step",
            "kata_workspace_bytes", "kata_scan_plan", "kata_host_plan", "kata_last_launch_count", "kata_last_impl",
            "kata_status_string",
            "kata_version")
@@ -59,6 +62,29 @@ class KataOpts(ctypes.Structure):
         ("s_init", ctypes.c_void_p),
         ("z_init", ctypes.c_void_p),
     ]
+
+
+class NormRopeArgs(ctypes.Structure):
+    _fields_ = ([("struct_size", ctypes.c_uint32)] + [(x, ctypes.c_int32) for x in ("B", "T", "H_q", "H_k", "d", "rotary_dim", "interleaved")] +
+                [("eps", ctypes.c_double), ("inv_freq", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("pos_stride", ctypes.c_int64 * 2),
+                 ("pos_offset", ctypes.c_int64)] + [(x, ctypes.c_void_p) for x in ("q", "k", "q_out", "k_out")] +
+                [(x, ctypes.c_int64 * 3) for x in ("q_stride", "k_stride", "q_out_stride", "k_out_stride")] +
+                [(x, ctypes.c_void_p) for x in ("q_weight", "k_weight", "dq", "dk")] + [(x, ctypes.c_int64 * 3) for x in ("dq_stride", "dk_stride")] +
+                [(x, ctypes.c_void_p) for x in ("dq_weight", "dk_weight")])
+
+
+class ShortConvArgs(ctypes.Structure):
+    _fields_ = ([("struct_size", ctypes.c_uint32)] + [(x, ctypes.c_int32) for x in ("B", "T", "D", "width", "silu")] +
+                [(x, ctypes.c_void_p) for x in ("x", "weight", "bias", "out")] + [(x, ctypes.c_int64 * 2) for x in ("x_stride", "out_stride")] +
+                [(x, ctypes.c_void_p) for x in ("s_init", "s_final", "lengths", "dout", "dx")] +
+                [(x, ctypes.c_int64 * 2) for x in ("dout_stride", "dx_stride")] + [(x, ctypes.c_void_p) for x in ("dweight", "dbias")])
+
+
+class SsmArgs(ctypes.Structure):
+    _fields_ = ([("struct_size", ctypes.c_uint32)] + [(x, ctypes.c_int32) for x in ("B", "T", "H", "G", "n", "d_v", "dt_softplus")] +
+                [(x, ctypes.c_void_p) for x in ("q", "k", "v", "dt", "out")] +
+                [(x, ctypes.c_int64 * 3) for x in ("q_stride", "k_stride", "v_stride", "dt_stride", "out_stride")] +
+                [(x, ctypes.c_void_p) for x in ("A", "D", "dt_bias", "s_init", "s_final", "lengths")])
 
 
 class KataError(RuntimeError):
@@ -91,6 +117,11 @@ def lib() -> ctypes.CDLL:
     L.kata_bwd_quadratic.restype = i
     L.kata_bwd_chunked.argtypes = [ptr] * 7 + [i] * 6 + [ctypes.POINTER(KataOpts)]
     L.kata_bwd_chunked.restype = i
+    for name, args in (("norm_rope", NormRopeArgs), ("short_conv", ShortConvArgs), ("ssm_scan", SsmArgs), ("ssm_step", SsmArgs)):
+        for form in ("fwd", "bwd", "decode"):
+            if hasattr(L, f"kata_{form}_{name}"):
+                f = getattr(L, f"kata_{form}_{name}")
+                f.argtypes, f.restype = [ctypes.POINTER(args), ctypes.POINTER(KataOpts)], i
     L.kata_workspace_bytes.argtypes = [i, i, i, i, i, i, i, ctypes.POINTER(KataOpts)]
     L.kata_workspace_bytes.restype = ctypes.c_size_t
     L.kata_scan_plan.argtypes = [i, i, i, i, i, i, i, ctypes.POINTER(KataOpts)] + [ctypes.POINTER(i)] * 3
@@ -541,4 +572,290 @@ def kata_chunk_state_scan_static(q, k, v, out, C: int = 64, *, scan_group: int =
                                             C, ctypes.byref(opts))
     if st != 0:
         raise KataError(st, "kata_chunk_state_scan_static")
+    return out
+
+
+# ---------------------------------------------------------------------------
+# rows around the attention and the decayed recurrence: tensors of any strides whose rows lie side by side
+# ---------------------------------------------------------------------------
+
+
+def _want(name: str, t, q, shape, dtype=None):
+    """ValueError unless t is a tensor of that shape and type on q's device whose innermost entries lie side by side."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a tensor")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} is {tuple(t.shape)}, the call needs {tuple(shape)}")
+    dtype = q.dtype if dtype is None else dtype
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} is {t.dtype}, the call needs {dtype}")
+    if not _on(t, q.device):
+        raise ValueError(f"{name} is on {t.device}, the call's tensors on {q.device}")
+    if t.dim() > 0 and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"the innermost entries of {name} must lie side by side")
+
+
+def _want_contiguous(name: str, t, q, shape, dtype=None):
+    _want(name, t, q, shape, dtype)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _want_main(name: str, t, dim: int):
+    if not isinstance(t, torch.Tensor) or t.dim() != dim:
+        raise ValueError(f"{name} must be a tensor of {dim} axes")
+    _dtype_code(t)
+    if t.numel() == 0:
+        raise ValueError(f"{name} has no elements")
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def _mixer_call(name: str, args, q, fn: int = -1, sizes=(), *, workspace=None, stream=None, impl: int = KATA_IMPL_AUTO, device_status=None):
+    """Calls entry point ``name`` on q's device; fn, sizes: the scratch to bring (fn < 0: none)."""
+    if q.device.type != "cuda":
+        raise ValueError(f"the tensors are on {q.device}, the call runs on a CUDA device")
+    if device_status is not None and (not isinstance(device_status, torch.Tensor) or device_status.nbytes < 4 or not _on(device_status, q.device)):
+        raise ValueError("device_status is one int32 on the device of the tensors")
+    if torch.cuda.current_device() != q.device.index:
+        with torch.cuda.device(q.device):
+            return _mixer_call(name, args, q, fn, sizes, workspace=workspace, stream=stream, impl=impl, device_status=device_status)
+    opts = make_opts(_dtype_code(q), impl=impl, stream=_stream(q.device) if stream is None else stream, device_status=_ptr(device_status) or 0)
+    held = _scratch(workspace, fn, sizes, opts, q.device) if fn >= 0 else None
+    args.struct_size = ctypes.sizeof(args)
+    st = getattr(lib(), name)(ctypes.byref(args), ctypes.byref(opts))
+    del held
+    if st != 0:
+        raise KataError(st, name)
+
+
+@functools.lru_cache(maxsize=64)
+def _frequencies(base: float, rotary_dim: int):
+    return (ctypes.c_double * max(1, rotary_dim // 2))(*(base ** (-2.0 * i / rotary_dim) for i in range(rotary_dim // 2)))
+
+
+def _rope_args(q, k, q_weight, k_weight, positions, offset, base, inv_freq, rotary_dim, interleaved, eps):
+    _want_main("q", q, 4)
+    B, H, T, d = q.shape
+    _want("q", q, q, q.shape)
+    if k is not None:
+        if not isinstance(k, torch.Tensor) or k.dim() != 4:
+            raise ValueError("k must be a tensor of 4 axes")
+        _want("k", k, q, (B, k.shape[1], T, d))
+    elif k_weight is not None:
+        raise ValueError("k_weight is set and k is not")
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            _want_contiguous(name, w, q, (d,))
+    if inv_freq is not None:
+        if isinstance(inv_freq, torch.Tensor):
+            if inv_freq.device.type != "cpu":
+                raise ValueError("inv_freq is a host sequence (it is read when the call is made)")
+            inv_freq = inv_freq.tolist()
+        if rotary_dim is None:
+            rotary_dim = 2 * len(inv_freq)
+        if len(inv_freq) != rotary_dim // 2:
+            raise ValueError(f"inv_freq has {len(inv_freq)} entries, the call needs {rotary_dim // 2}")
+        freq = (ctypes.c_double * max(1, len(inv_freq)))(*inv_freq)
+    else:
+        rotary_dim = d if rotary_dim is None else rotary_dim
+        freq = _frequencies(float(base), int(rotary_dim))
+    a = NormRopeArgs(B=B, T=T, H_q=H, H_k=k.shape[1] if k is not None else 0, d=d, rotary_dim=rotary_dim, interleaved=int(bool(interleaved)), eps=eps,
+                     inv_freq=ctypes.addressof(freq), pos_offset=offset, q=q.data_ptr(), k=_ptr(k), q_weight=_ptr(q_weight), k_weight=_ptr(k_weight))
+    a.freq = freq                                        # (held as long as the arguments)
+    a.q_stride[:] = q.stride()[:3]
+    if k is not None:
+        a.k_stride[:] = k.stride()[:3]
+    if positions is not None:
+        if not isinstance(positions, torch.Tensor) or tuple(positions.shape) not in ((T,), (B, T)):
+            raise ValueError(f"positions must be {(T,)} or {(B, T)}")
+        if positions.dtype is not torch.int64 or not _on(positions, q.device):
+            raise ValueError("positions are int64 on the device of q")
+        a.positions = positions.data_ptr()
+        a.pos_stride[:] = (positions.stride(0) if positions.dim() == 2 else 0, positions.stride(-1))
+    return a
+
+
+def kata_fwd_norm_rope(q, k=None, q_weight=None, k_weight=None, positions=None, *, offset: int = 0, base: float = 10000.0, inv_freq=None,
+                       rotary_dim: Optional[int] = None, interleaved: bool = False, eps: float = 1e-6, q_out=None, k_out=None, stream=None):
+    """Norm of every row of q [B,H,T,d] and k [B,H_k,T,d] (or None) by its root mean square, times the weights [d] (or None), and
+    rotation by the token's position (int64 [T] or [B,T], or offset + t).  q, k: any strides whose rows lie side by side, such as
+    views of a projection.  inv_freq: angles per position, a host sequence of rotary_dim / 2 (else base^(-2i / rotary_dim)).
+    Returns (q_out, k_out), contiguous [B,H,T,d] unless given."""
+    a = _rope_args(q, k, q_weight, k_weight, positions, offset, base, inv_freq, rotary_dim, interleaved, eps)
+    outs = []
+    for name, x, out in (("q_out", q, q_out), ("k_out", k, k_out)):
+        if x is None and out is not None:
+            raise ValueError(f"{name} is set and k is not")
+        if x is not None and out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        elif x is not None:
+            _want(name, out, q, x.shape)
+        outs.append(out)
+        if out is not None:
+            setattr(a, name, out.data_ptr())
+            getattr(a, name + "_stride")[:] = out.stride()[:3]
+    _mixer_call("kata_fwd_norm_rope", a, q, stream=stream)
+    return tuple(outs)
+
+
+def kata_bwd_norm_rope(dq_out, dk_out, q, k=None, q_weight=None, k_weight=None, positions=None, *, offset: int = 0, base: float = 10000.0,
+                       inv_freq=None, rotary_dim: Optional[int] = None, interleaved: bool = False, eps: float = 1e-6, dq=None, dk=None,
+                       workspace: Optional[Workspace] = None, stream=None):
+    """Gradients of ``kata_fwd_norm_rope`` from those of its outputs: (dq, dk, dq_weight, dk_weight).  dq and dk take the layout of
+    q and k unless given; the weights' gradients are fp32 [d] (None without a weight)."""
+    a = _rope_args(q, k, q_weight, k_weight, positions, offset, base, inv_freq, rotary_dim, interleaved, eps)
+    grads, sums = [], []
+    for name, x, g, dx, w in (("q", q, dq_out, dq, q_weight), ("k", k, dk_out, dk, k_weight)):
+        if x is None:
+            if g is not None or dx is not None:
+                raise ValueError("gradients of k are set and k is not")
+            grads.append(None)
+            sums.append(None)
+            continue
+        _want(f"d{name}_out", g, q, x.shape)
+        if dx is None:
+            dx = torch.empty_like(x)
+        _want(f"d{name}", dx, q, x.shape)
+        dw = torch.empty(x.shape[-1], dtype=torch.float32, device=x.device) if w is not None else None
+        setattr(a, f"{name}_out", g.data_ptr())
+        getattr(a, f"{name}_out_stride")[:] = g.stride()[:3]
+        setattr(a, f"d{name}", dx.data_ptr())
+        getattr(a, f"d{name}_stride")[:] = dx.stride()[:3]
+        setattr(a, f"d{name}_weight", _ptr(dw))
+        grads.append(dx)
+        sums.append(dw)
+    B, H, T, d = q.shape
+    _mixer_call("kata_bwd_norm_rope", a, q, KATA_FN_BWD_NORM_ROPE, (B, H + a.H_k, T, d, 0, 0), workspace=workspace, stream=stream)
+    return (*grads, *sums)
+
+
+def _conv_args(x, weight, bias, silu, s_init, s_final, lengths):
+    _want_main("x", x, 3)
+    B, T, D = x.shape
+    _want("x", x, x, x.shape)
+    if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
+        raise ValueError("weight must be a tensor of 2 axes")
+    W = weight.shape[1]
+    _want_contiguous("weight", weight, x, (D, W))
+    if bias is not None:
+        _want_contiguous("bias", bias, x, (D,))
+    for name, s in (("s_init", s_init), ("s_final", s_final)):
+        if s is not None:
+            _want_contiguous(name, s, x, (B, D, W - 1))
+    if lengths is not None:
+        _want_contiguous("lengths", lengths, x, (B,), torch.int32)
+    a = ShortConvArgs(B=B, T=T, D=D, width=W, silu=int(bool(silu)), x=x.data_ptr(), weight=weight.data_ptr(), bias=_ptr(bias), s_init=_ptr(s_init),
+                      s_final=_ptr(s_final), lengths=_ptr(lengths))
+    a.x_stride[:] = x.stride()[:2]
+    return a
+
+
+def kata_fwd_short_conv(x, weight, bias=None, *, silu: bool = False, s_init=None, s_final=None, lengths=None, out=None, stream=None):
+    """Causal convolution of x [B,T,D] along T with weight [D,width], bias [D] and optionally z * sigmoid(z).  s_init, s_final
+    [B,D,width-1]: the inputs before the first and up to the last token (may be one tensor); lengths: int32 [B] of a padded
+    batch.  Returns out [B,T,D], contiguous unless given."""
+    a = _conv_args(x, weight, bias, silu, s_init, s_final, lengths)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        _want("out", out, x, x.shape)
+    a.out = out.data_ptr()
+    a.out_stride[:] = out.stride()[:2]
+    _mixer_call("kata_fwd_short_conv", a, x, stream=stream)
+    return out
+
+
+def kata_decode_short_conv(x, weight, state, bias=None, *, silu: bool = False, out=None, stream=None):
+    """One token of every sequence: x [B,D]; state [B,D,width-1] is moved on in place.  Returns out [B,D]."""
+    _want_main("x", x, 2)
+    a = _conv_args(x[:, None], weight, bias, silu, state, state, None)
+    if state is None:
+        raise ValueError("state must be a tensor")
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        _want("out", out, x, x.shape)
+    a.out = out.data_ptr()
+    a.out_stride[:] = (out.stride(0), 0)
+    _mixer_call("kata_decode_short_conv", a, x, stream=stream)
+    return out
+
+
+def kata_bwd_short_conv(dout, x, weight, bias=None, *, silu: bool = False, lengths=None, dx=None, workspace: Optional[Workspace] = None, stream=None):
+    """Gradients of ``kata_fwd_short_conv`` (without states): (dx, dweight [D,width] fp32, dbias [D] fp32 or None)."""
+    a = _conv_args(x, weight, bias, silu, None, None, lengths)
+    _want("dout", dout, x, x.shape)
+    if dx is None:
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        _want("dx", dx, x, x.shape)
+    dweight = torch.empty(weight.shape, dtype=torch.float32, device=x.device)
+    dbias = torch.empty(bias.shape, dtype=torch.float32, device=x.device) if bias is not None else None
+    a.dout, a.dx, a.dweight, a.dbias = dout.data_ptr(), dx.data_ptr(), dweight.data_ptr(), _ptr(dbias)
+    a.dout_stride[:] = dout.stride()[:2]
+    a.dx_stride[:] = dx.stride()[:2]
+    B, T, D = x.shape
+    _mixer_call("kata_bwd_short_conv", a, x, KATA_FN_BWD_SHORT_CONV, (B, D, T, a.width, 0, 0), workspace=workspace, stream=stream)
+    return dx, dweight, dbias
+
+
+def _ssm_args(q, k, v, dt, A, D, dt_bias, dt_softplus, lengths, out):
+    """Of tensors with a token axis; ``out`` None: a new tensor in the layout of v."""
+    _want_main("v", v, 4)
+    B, H, T, d_v = v.shape
+    if not isinstance(q, torch.Tensor) or q.dim() != 4:
+        raise ValueError("q must be a tensor of 4 axes")
+    G, n = q.shape[1], q.shape[3]
+    _want("v", v, v, v.shape)
+    _want("q", q, v, (B, G, T, n))
+    _want("k", k, v, (B, G, T, n))
+    if not isinstance(dt, torch.Tensor) or tuple(dt.shape) != (B, H, T) or dt.dtype is not v.dtype or not _on(dt, v.device):
+        raise ValueError(f"dt must be {(B, H, T)} in the type and on the device of v")
+    for name, x in (("A", A), ("D", D), ("dt_bias", dt_bias)):
+        if x is not None or name == "A":
+            _want_contiguous(name, x, v, (H,), torch.float32)
+    if lengths is not None:
+        _want_contiguous("lengths", lengths, v, (B,), torch.int32)
+    if out is None:
+        out = torch.empty_like(v)
+    _want("out", out, v, v.shape)
+    a = SsmArgs(B=B, T=T, H=H, G=G, n=n, d_v=d_v, dt_softplus=int(bool(dt_softplus)), q=q.data_ptr(), k=k.data_ptr(), v=v.data_ptr(),
+                dt=dt.data_ptr(), out=out.data_ptr(), A=A.data_ptr(), D=_ptr(D), dt_bias=_ptr(dt_bias), lengths=_ptr(lengths))
+    for name, x in (("q", q), ("k", k), ("v", v), ("dt", dt), ("out", out)):
+        getattr(a, name + "_stride")[:] = x.stride()[:3]
+    return a, out
+
+
+def kata_fwd_ssm_scan(q, k, v, dt, A, D=None, dt_bias=None, *, dt_softplus: bool = False, s_init=None, s_final=None, lengths=None, out=None,
+                      workspace: Optional[Workspace] = None, stream=None, impl: int = KATA_IMPL_AUTO, device_status=None):
+    """Selective state space scan: S_t = exp(s_t A) S_{t-1} + s_t k_t v_t^T, out_t = S_t^T q_t + D v_t, s_t = dt_t + dt_bias (or its
+    softplus).  q, k [B,G,T,n]; v [B,H,T,d_v]; dt [B,H,T]; A, D, dt_bias [H] fp32; s_init, s_final [B,H,n,d_v] fp32, the states
+    before the first and after the last token (may be one tensor); lengths: int32 [B] of a padded batch.  Strided views are
+    taken as they are; out takes the layout of v unless given."""
+    a, out = _ssm_args(q, k, v, dt, A, D, dt_bias, dt_softplus, lengths, out)
+    for name, s in (("s_init", s_init), ("s_final", s_final)):
+        if s is not None:
+            _want_contiguous(name, s, v, (a.B, a.H, a.n, a.d_v), torch.float32)
+            setattr(a, name, s.data_ptr())
+    _mixer_call("kata_fwd_ssm_scan", a, v, KATA_FN_SSM_SCAN, (a.B, a.H, a.T, a.n, a.d_v, 0), workspace=workspace, stream=stream, impl=impl,
+                device_status=device_status)
+    return out
+
+
+def kata_decode_ssm_step(q, k, v, dt, A, state, D=None, dt_bias=None, *, dt_softplus: bool = False, out=None, stream=None):
+    """One token of the scan for every head: q, k [B,G,n]; v [B,H,d_v]; dt [B,H]; state [B,H,n,d_v] fp32 is moved on in place.
+    Returns out [B,H,d_v]."""
+    for name, x, dim in (("q", q, 3), ("k", k, 3), ("v", v, 3), ("dt", dt, 2)):
+        if not isinstance(x, torch.Tensor) or x.dim() != dim:
+            raise ValueError(f"{name} must be a tensor of {dim} axes")
+    if out is None:
+        out = torch.empty_like(v)
+    _want("out", out, v, v.shape)
+    a, _ = _ssm_args(q[:, :, None], k[:, :, None], v[:, :, None], dt[:, :, None], A, D, dt_bias, dt_softplus, None, out[:, :, None])
+    _want_contiguous("state", state, v, (a.B, a.H, a.n, a.d_v), torch.float32)
+    a.s_init = a.s_final = state.data_ptr()
+    _mixer_call("kata_decode_ssm_step", a, v, stream=stream)
     return out

@@ -734,6 +734,26 @@ int host_pipelined(const Prepared& r, const PipePlan& pp, const void* q_host, co
 }
 
 }  // namespace
+
+int read_call_opts(const kata_opts* opts, CallOpts& out) {
+  if (opts == nullptr || opts->struct_size != sizeof(kata_opts)) return KATA_ERR_INVALID_ARG;
+  if (opts->dtype != KATA_F32 && opts->dtype != KATA_BF16) return KATA_ERR_INVALID_ARG;
+  if (opts->impl < KATA_IMPL_AUTO || opts->impl > KATA_IMPL_TENSOR) return KATA_ERR_INVALID_ARG;
+  if (opts->s_pre != nullptr || opts->z_pre != nullptr || opts->s_init != nullptr || opts->z_init != nullptr) return KATA_ERR_INVALID_ARG;
+  out = CallOpts{opts->dtype, opts->impl, opts->workspace, opts->workspace_bytes, opts->device_status, static_cast<cudaStream_t>(opts->stream)};
+  return KATA_OK;
+}
+
+int check_device() { return check_arch(); }
+
+int finish_call(const LaunchCtx& ctx, int impl) {
+  if (ctx.status == KATA_OK) {
+    g_last_launches = ctx.launches;
+    g_last_impl = impl;
+  }
+  return ctx.status;
+}
+
 }  // namespace kata
 
 using namespace kata;
@@ -920,6 +940,7 @@ int kata_bwd_chunked(const void* q, const void* k, const void* v, const void* do
 size_t kata_workspace_bytes(int fn, int B, int H, int T, int d_k, int d_v, int C, const kata_opts* opts) {
   const bool host_io = (fn & KATA_FN_HOST_IO) != 0;
   fn &= ~KATA_FN_HOST_IO;
+  if (fn >= KATA_FN_SSM_SCAN && fn <= KATA_FN_BWD_SHORT_CONV) return host_io ? 0 : mixer_workspace_bytes(fn, B, H, T, d_k, d_v, opts);
   if (fn == KATA_FN_BWD_CHUNKED) {
     Opts o;
     if (host_io || read_opts(opts, o) != KATA_OK || B < 1 || H < 1 || T < 1 || C != kChunk) return 0;

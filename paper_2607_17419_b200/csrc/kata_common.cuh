@@ -252,4 +252,75 @@ int tc_order1_tile();
 void tc_order1(const Problem& p, const ScanPlan& plan, bool use_scan, int C, float* ws, int* device_status,
                LaunchCtx& ctx);
 
+// ---- rows around the attention and the decayed recurrence (kata_mixer_api.cu) ----
+// What kata_api.cu does for every entry point: options of a call that takes no state pointers, the architecture check and the
+// report of a call that succeeded.
+struct CallOpts {
+  int dtype, impl;
+  void* workspace;
+  size_t workspace_bytes;
+  int* device_status;
+  cudaStream_t stream;
+};
+int read_call_opts(const kata_opts* o, CallOpts& out);
+int check_device();
+int finish_call(const LaunchCtx& ctx, int impl);
+size_t mixer_workspace_bytes(int fn, int B, int H, int T, int d_k, int d_v, const kata_opts* opts);   // the functions of kata_mixer_api.cu
+
+// A tensor as the kernels see it: strides in elements of the axes before the innermost.
+struct View {
+  char* p;
+  long long s0, s1, s2;
+};
+
+struct NormRope {
+  int B, T, Hq, Hk, d, rot, dtype;
+  bool interleaved;
+  float eps;
+  const long long* positions;
+  long long ps0, ps1, pos_offset;
+  View q, k, q_out, k_out, dq, dk;
+  const void *q_weight, *k_weight;
+  float *dq_weight, *dk_weight;
+  unsigned long long turns[64];      // inv_freq / 2 pi as fractions of a turn, 64-bit fixed point
+};
+void norm_rope_fwd(const NormRope& a, LaunchCtx& ctx);
+size_t norm_rope_bwd_workspace_elems(int B, int T, int H, int d);
+void norm_rope_bwd(const NormRope& a, float* ws, LaunchCtx& ctx);
+
+struct ShortConv {
+  int B, T, D, W, dtype;
+  bool silu;
+  const void *weight, *bias;
+  View x, out, dout, dx;             // s0 batch, s1 token
+  const void* s_init;
+  void* s_final;
+  const int* lengths;
+  float *dweight, *dbias;
+};
+void short_conv_fwd(const ShortConv& a, LaunchCtx& ctx);
+size_t short_conv_bwd_workspace_elems(int B, int T, int D, int W);
+void short_conv_bwd(const ShortConv& a, float* ws, LaunchCtx& ctx);
+
+struct Ssm {
+  int B, T, H, G, n, d, dtype;
+  bool softplus;
+  View q, k, v, dt, out;             // s0 batch, s1 head or group, s2 token
+  const float *A, *D, *dt_bias;
+  const float* s_init;
+  float* s_final;
+  const int* lengths;
+};
+void ssm_step(const Ssm& a, LaunchCtx& ctx);
+// Segments of the token axis: their own states [BH][segments - 1][n][d] and decays [BH][segments - 1] are in ws.
+struct SsmPlan {
+  int segments, seg_tokens;
+};
+SsmPlan ssm_plan(int BH, int T, int n, int d, bool tensor);
+size_t ssm_workspace_bytes(int BH, int n, int d, const SsmPlan& plan);
+void ssm_prefix(const Ssm& a, const SsmPlan& plan, float* ws, LaunchCtx& ctx);
+void simt_ssm(const Ssm& a, const SsmPlan& plan, float* ws, LaunchCtx& ctx);
+bool tc_ssm_supported(int dtype, int n, int d);
+void tc_ssm(const Ssm& a, const SsmPlan& plan, float* ws, int* device_status, LaunchCtx& ctx);
+
 }  // namespace kata

@@ -1,0 +1,229 @@
+// Selective state space scan token by token in fp32 (every element type and size), and the sum over the segments of a head.
+//   S <- a_t S + s_t k_t v_t^T,  o_t = S^T q_t + D v_t
+// One CTA per head and segment of the tokens, the state in registers: a thread has one column and a quarter of the rows.  Tokens are
+// staged 16 at a time (s_t folded into the keys), the next 16 on their way meanwhile; the four sums of an output meet in shared
+// memory.  Bound by fp32 issue: three operations per state entry and token.
+// Few heads: the token axis is cut into segments.  Their own states (from zero) come first, ssm_prefix turns them into the states
+// before the segments, and the second pass starts from those.
+#include "kata_rows.cuh"
+#include "kata_ssm.cuh"
+
+namespace kata {
+namespace {
+
+constexpr int TB = 16;                 // tokens staged at a time
+constexpr int RG = 4;                  // threads that share a column
+
+template <typename T, int N, int DV, bool STATE>
+__global__ void __launch_bounds__(DV * RG) simt_ssm_kernel(const __grid_constant__ Ssm a, const SsmPlan plan, float* __restrict__ ws) {
+  constexpr int THREADS = DV * RG, R = N / RG, E = 16 / sizeof(T);
+  constexpr int NQ = (TB * N / E + THREADS - 1) / THREADS, NV = (TB * DV / E + THREADS - 1) / THREADS;
+  __shared__ __align__(16) float ks[TB][N], qs[STATE ? 1 : TB][N], vs[TB][DV], part[STATE ? 1 : TB][RG][DV];
+  __shared__ float as[TB];
+  wait_for_kernels_ahead();
+  const int bh = blockIdx.x / plan.segments, seg = blockIdx.x % plan.segments;
+  if (STATE && seg + 1 == plan.segments) return;
+  const int b = bh / a.H, h = bh - b * a.H, g = h / (a.H / a.G), tid = threadIdx.x, col = tid % DV, rg = tid / DV;
+  const int len = sequence_length(a.lengths, b, a.T);
+  const int t0 = seg * plan.seg_tokens, t1 = min(t0 + plan.seg_tokens, a.T), live = min(t1, len);
+  const T* kp = reinterpret_cast<const T*>(a.k.p) + b * a.k.s0 + g * a.k.s1;
+  const T* qp = reinterpret_cast<const T*>(a.q.p) + b * a.q.s0 + g * a.q.s1;
+  const T* vp = reinterpret_cast<const T*>(a.v.p) + b * a.v.s0 + h * a.v.s1;
+  const T* dp = reinterpret_cast<const T*>(a.dt.p) + b * a.dt.s0 + h * a.dt.s1;
+  T* op = reinterpret_cast<T*>(a.out.p) + b * a.out.s0 + h * a.out.s1;
+  const float A = a.A[h], skip = a.D != nullptr ? a.D[h] : 0.f;
+  constexpr size_t SE = (size_t)N * DV;
+  float S[R];
+  const float* init = STATE ? nullptr : plan.segments > 1 ? ws + ssm_slot(plan.segments, bh, seg) * SE : a.s_init != nullptr ? a.s_init + (size_t)bh * SE : nullptr;
+#pragma unroll
+  for (int r = 0; r < R; ++r) S[r] = init != nullptr ? init[(rg * R + r) * DV + col] : 0.f;
+  Entries<T, E> kr[NQ], qr[NQ], vr[NV];
+  float dr = 0.f;
+  auto fetch = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      const int e = (tid + i * THREADS) * E, row = t + e / N;
+      kr[i].zero();
+      qr[i].zero();
+      if (e < TB * N && row < live) {
+        kr[i].load(kp + row * a.k.s2 + e % N);
+        if (!STATE) qr[i].load(qp + row * a.q.s2 + e % N);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int e = (tid + i * THREADS) * E, row = t + e / DV;
+      vr[i].zero();
+      if (e < TB * DV && row < live) vr[i].load(vp + row * a.v.s2 + e % DV);
+    }
+    if (tid < TB && t + tid < live) dr = to_f32<T>(dp[(t + tid) * a.dt.s2]);
+  };
+  __shared__ float ss[TB];
+  double decay = 0.0;                  // log of the decay over the segment, this thread's tokens
+  if (t0 < live) fetch(t0);
+  for (int t = t0; t < live; t += TB) {
+    __syncthreads();
+    if (tid < TB) {
+      const float s = t + tid < live ? ssm_step_size(a, dr, h) : 0.f;
+      ss[tid] = s;
+      as[tid] = expf(s * A);
+      if (STATE) decay += (double)s * A;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      const int e = (tid + i * THREADS) * E;
+      if (e < TB * N) {
+        float x[E];
+        kr[i].get(x);
+        const float s = ss[e / N];
+#pragma unroll
+        for (int j = 0; j < E; ++j) ks[e / N][e % N + j] = s * x[j];
+        if (!STATE) {
+          qr[i].get(x);
+#pragma unroll
+          for (int j = 0; j < E; ++j) qs[e / N][e % N + j] = x[j];
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int e = (tid + i * THREADS) * E;
+      if (e < TB * DV) {
+        float x[E];
+        vr[i].get(x);
+#pragma unroll
+        for (int j = 0; j < E; ++j) vs[e / DV][e % DV + j] = x[j];
+      }
+    }
+    __syncthreads();
+    if (t + TB < live) fetch(t + TB);
+#pragma unroll 2
+    for (int u = 0; u < TB; ++u) {
+      const float v = vs[u][col], d = as[u];
+      float y = 0.f;
+#pragma unroll
+      for (int r = 0; r < R; r += 4) {
+        const float4 k4 = *reinterpret_cast<const float4*>(&ks[u][rg * R + r]);
+        S[r] = fmaf(d, S[r], k4.x * v);
+        S[r + 1] = fmaf(d, S[r + 1], k4.y * v);
+        S[r + 2] = fmaf(d, S[r + 2], k4.z * v);
+        S[r + 3] = fmaf(d, S[r + 3], k4.w * v);
+        if (!STATE) {
+          const float4 q4 = *reinterpret_cast<const float4*>(&qs[u][rg * R + r]);
+          y = fmaf(q4.x, S[r], y);
+          y = fmaf(q4.y, S[r + 1], y);
+          y = fmaf(q4.z, S[r + 2], y);
+          y = fmaf(q4.w, S[r + 3], y);
+        }
+      }
+      if (!STATE) part[u][rg][col] = y;
+    }
+    if (!STATE) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < TB / RG; ++i) {
+        const int u = i * RG + rg;
+        if (t + u < live)
+          op[(t + u) * a.out.s2 + col] = from_f32<T>(fmaf(skip, vs[u][col], (part[u][0][col] + part[u][1][col]) + (part[u][2][col] + part[u][3][col])));
+      }
+    }
+  }
+  if constexpr (STATE) {
+    float* to = ws + ssm_slot(plan.segments, bh, seg + 1) * SE;
+#pragma unroll
+    for (int r = 0; r < R; ++r) to[(rg * R + r) * DV + col] = S[r];
+    if (tid < 32) {
+      if (tid >= TB) decay = 0.0;
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1) decay += __shfl_xor_sync(0xffffffffu, decay, off);
+      if (tid == 0) ws[(size_t)a.B * a.H * plan.segments * SE + ssm_slot(plan.segments, bh, seg)] = expf((float)decay);
+    }
+  } else {
+    for (int t = max(live, t0) + rg; t < t1; t += RG) op[t * a.out.s2 + col] = from_f32<T>(0.f);
+    if (a.s_final != nullptr && seg + 1 == plan.segments) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) a.s_final[(size_t)bh * SE + (rg * R + r) * DV + col] = S[r];
+    }
+  }
+}
+
+// Slot j of a head: from the own state of segment j - 1 to the state before segment j (slot 0: the state handed in).
+__global__ void __launch_bounds__(128) ssm_prefix_kernel(float* __restrict__ ws, const float* __restrict__ s_init, int BH, int segments, int se) {
+  wait_for_kernels_ahead();
+  constexpr int U = 8;
+  const int bh = blockIdx.y, e = blockIdx.x * 128 + threadIdx.x;           // (n d_v is a multiple of 128)
+  float* s = ws + ssm_slot(segments, bh, 0) * se + e;
+  const float* decay = ws + (size_t)BH * segments * se + ssm_slot(segments, bh, 0);
+  float cur = s_init != nullptr ? s_init[(size_t)bh * se + e] : 0.f;
+  s[0] = cur;
+  for (int j = 1; j < segments; j += U) {
+    float own[U], d[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (j + u < segments) {
+        own[u] = s[(size_t)(j + u) * se];
+        d[u] = decay[j + u - 1];
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (j + u < segments) {
+        cur = fmaf(d[u], cur, own[u]);
+        s[(size_t)(j + u) * se] = cur;
+      }
+  }
+}
+
+template <typename T, int N, int DV> void launch(const Ssm& a, const SsmPlan& plan, float* ws, LaunchCtx& ctx) {
+  const dim3 grid((unsigned)(a.B * a.H) * plan.segments);
+  if (plan.segments > 1) {
+    launch_after(ctx, simt_ssm_kernel<T, N, DV, true>, grid, dim3(DV * RG), 0, a, plan, ws);
+    ssm_prefix(a, plan, ws, ctx);
+  }
+  launch_after(ctx, simt_ssm_kernel<T, N, DV, false>, grid, dim3(DV * RG), 0, a, plan, ws);
+}
+
+template <typename T, int N> void by_width(const Ssm& a, const SsmPlan& plan, float* ws, LaunchCtx& ctx) {
+  if (a.d == 16) launch<T, N, 16>(a, plan, ws, ctx);
+  else if (a.d == 32) launch<T, N, 32>(a, plan, ws, ctx);
+  else launch<T, N, 64>(a, plan, ws, ctx);
+}
+
+template <typename T> void by_rows(const Ssm& a, const SsmPlan& plan, float* ws, LaunchCtx& ctx) {
+  if (a.n == 16) by_width<T, 16>(a, plan, ws, ctx);
+  else if (a.n == 32) by_width<T, 32>(a, plan, ws, ctx);
+  else if (a.n == 64) by_width<T, 64>(a, plan, ws, ctx);
+  else by_width<T, 128>(a, plan, ws, ctx);
+}
+
+}  // namespace
+
+// Segments: while the heads alone leave SMs idle, as many as fill them, of at least 256 tokens.
+SsmPlan ssm_plan(int BH, int T, int n, int d, bool tensor) {
+  const int wanted = (tensor ? 2 : 4) * kPlanSMs / BH;
+  SsmPlan p{1, T};
+  if (wanted < 2 || T < 512) return p;
+  int tokens = (T + wanted - 1) / wanted;
+  tokens = (tokens + 127) / 128 * 128;
+  p.seg_tokens = tokens < 256 ? 256 : tokens;
+  p.segments = (T + p.seg_tokens - 1) / p.seg_tokens;
+  return p;
+}
+
+size_t ssm_workspace_bytes(int BH, int n, int d, const SsmPlan& plan) {
+  return plan.segments > 1 ? (size_t)BH * plan.segments * ((size_t)n * d + 1) * sizeof(float) : 0;
+}
+
+void ssm_prefix(const Ssm& a, const SsmPlan& plan, float* ws, LaunchCtx& ctx) {
+  launch_after(ctx, ssm_prefix_kernel, dim3(a.n * a.d / 128, a.B * a.H), dim3(128), 0, ws, a.s_init, a.B * a.H, plan.segments, a.n * a.d);
+}
+
+void simt_ssm(const Ssm& a, const SsmPlan& plan, float* ws, LaunchCtx& ctx) {
+  if (a.dtype == KATA_F32) by_rows<float>(a, plan, ws, ctx);
+  else by_rows<__nv_bfloat16>(a, plan, ws, ctx);
+}
+
+bool tc_ssm_supported(int dtype, int n, int d) { return false; }
+void tc_ssm(const Ssm& a, const SsmPlan& plan, float* ws, int* device_status, LaunchCtx& ctx) {}
+
+}  // namespace kata
