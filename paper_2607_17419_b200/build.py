@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkata.so")
 HOST = os.path.join(HERE, "_kata_torch.so")      # the binding's tensor calls (csrc/kata_torch.cpp)
 SOURCES = ["kata_api.cu", "kata_simt_quadratic.cu", "kata_simt_bwd.cu", "kata_simt_bwd_chunked.cu", "kata_simt_chunked.cu", "kata_simt_order1.cu", "kata_simt_attend.cu", "kata_tc.cu", "kata_tc_chunked.cu",
-    "kata_tc_stream.cu", "kata_tc_stream_export.cu", "kata_tc_stream_restart.cu", "kata_tc_stream_state.cu", "kata_tc_attend.cu", "kata_tc_state.cu", "kata_tc_bwd.cu", "kata_tc_order1.cu", "kata_decode.cu", "kata_mixer_api.cu", "kata_norm_rope.cu", "kata_short_conv.cu", "kata_simt_ssm.cu", "kata_ssm_step.cu", "kata_static.cu", "kata_selftest.cu"]
+    "kata_tc_stream.cu", "kata_tc_stream_export.cu", "kata_tc_stream_restart.cu", "kata_tc_stream_state.cu", "kata_tc_attend.cu", "kata_tc_state.cu", "kata_tc_bwd.cu", "kata_tc_order1.cu", "kata_decode.cu", "kata_mixer_api.cu", "kata_norm_rope.cu", "kata_short_conv.cu", "kata_simt_ssm.cu", "kata_ssm_step.cu", "kata_static.cu", "kata_tc_ssm.cu", "kata_selftest.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "--use_fast_math=false"]
 

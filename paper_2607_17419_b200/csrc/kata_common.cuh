@@ -312,13 +312,15 @@ struct Ssm {
   const int* lengths;
 };
 void ssm_step(const Ssm& a, LaunchCtx& ctx);
-// Segments of the token axis: their own states [BH][segments - 1][n][d] and decays [BH][segments - 1] are in ws.
+// Segments of the token axis.  In ws, with more than one of them or a final state wanted of the tensor-core kernels: slots
+// [BH][slots][n][d], slot j the state before segment j (until the prefix is formed, slot j + 1 holds the own state of segment j), and
+// the decays over the segments [BH][slots].  slots = segments, and one more for a final state.
 struct SsmPlan {
   int segments, seg_tokens;
 };
-SsmPlan ssm_plan(int BH, int T, int n, int d, bool tensor);
-size_t ssm_workspace_bytes(int BH, int n, int d, const SsmPlan& plan);
-void ssm_prefix(const Ssm& a, const SsmPlan& plan, float* ws, LaunchCtx& ctx);
+SsmPlan ssm_plan(int BH, int T, bool tensor);
+size_t ssm_workspace_bytes(int BH, int n, int d, int slots);
+void ssm_prefix(const Ssm& a, const SsmPlan& plan, int slots, float* ws, LaunchCtx& ctx);
 void simt_ssm(const Ssm& a, const SsmPlan& plan, float* ws, LaunchCtx& ctx);
 bool tc_ssm_supported(int dtype, int n, int d);
 void tc_ssm(const Ssm& a, const SsmPlan& plan, float* ws, int* device_status, LaunchCtx& ctx);

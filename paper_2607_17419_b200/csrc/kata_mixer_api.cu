@@ -155,6 +155,12 @@ int ssm_shape(int B, int H, int T, int n, int d) {
 
 bool ssm_tensor(const CallOpts& o, int n, int d) { return o.impl != KATA_IMPL_SIMT && tc_ssm_supported(o.dtype, n, d); }
 
+// Slots of states in the scratch (see SsmPlan).
+int ssm_slots(const SsmPlan& plan, bool tensor, bool final_state) {
+  const int more = tensor && final_state ? 1 : 0;
+  return plan.segments + more > 1 ? plan.segments + more : 0;
+}
+
 int ssm(const kata_ssm_args* a, const kata_opts* opts, bool step) {
   CallOpts o;
   KATA_TRY(read_call_opts(opts, o));
@@ -162,7 +168,7 @@ int ssm(const kata_ssm_args* a, const kata_opts* opts, bool step) {
   const int T = step ? 1 : a->T;
   KATA_TRY(ssm_shape(a->B, a->H, T, a->n, a->d_v));
   if (a->G < 1 || a->H % a->G != 0) return KATA_ERR_INVALID_ARG;
-  const bool tensor = !step && ssm_tensor(o, a->n, a->d_v);
+  bool tensor = !step && ssm_tensor(o, a->n, a->d_v);
   if (o.impl == KATA_IMPL_TENSOR && !tensor) return KATA_ERR_UNSUPPORTED_SHAPE;
   if (a->A == nullptr || a->dt == nullptr) return KATA_ERR_INVALID_ARG;
   if (step && (a->s_init == nullptr || a->s_final != a->s_init || a->lengths != nullptr)) return KATA_ERR_INVALID_ARG;
@@ -185,8 +191,13 @@ int ssm(const kata_ssm_args* a, const kata_opts* opts, bool step) {
   for (const void* p : {(const void*)a->A, (const void*)a->D, (const void*)a->dt_bias, (const void*)a->lengths})
     if ((reinterpret_cast<uintptr_t>(p) & 3u) != 0) return KATA_ERR_ALIGNMENT;
   if ((reinterpret_cast<uintptr_t>(a->s_init) & 15u) != 0 || (reinterpret_cast<uintptr_t>(a->s_final) & 15u) != 0) return KATA_ERR_ALIGNMENT;
-  const SsmPlan plan = step ? SsmPlan{1, 1} : ssm_plan(a->B * a->H, T, a->n, a->d_v, tensor);
-  KATA_TRY(check_workspace(o, align_up(ssm_workspace_bytes(a->B * a->H, a->n, a->d_v, plan))));
+  const SsmPlan plan = step ? SsmPlan{1, 1} : ssm_plan(a->B * a->H, T, tensor);
+  if (tensor && T > 1 && (r.q.s2 == 0 || r.k.s2 == 0 || r.v.s2 == 0)) {      // (one row for all tokens has no tensor map)
+    if (o.impl == KATA_IMPL_TENSOR) return KATA_ERR_UNSUPPORTED_SHAPE;
+    tensor = false;
+  }
+  const int slots = ssm_slots(plan, tensor, r.s_final != nullptr);
+  KATA_TRY(check_workspace(o, align_up(ssm_workspace_bytes(a->B * a->H, a->n, a->d_v, slots))));
   KATA_TRY(check_device());
   LaunchCtx ctx{o.stream, 0, KATA_OK};
   float* ws = static_cast<float*>(o.workspace);
@@ -205,7 +216,8 @@ size_t mixer_workspace_bytes(int fn, int B, int H, int T, int d_k, int d_v, cons
   if (fn == KATA_FN_BWD_SHORT_CONV)
     return d_k >= 2 && d_k <= 4 && H <= (1 << 24) && (double)B * T * H <= 1e11 ? align_up(short_conv_bwd_workspace_elems(B, T, H, d_k) * sizeof(float)) : 0;
   if (ssm_shape(B, H, T, d_k, d_v) != KATA_OK) return 0;
-  return align_up(ssm_workspace_bytes(B * H, d_k, d_v, ssm_plan(B * H, T, d_k, d_v, ssm_tensor(o, d_k, d_v))));
+  const bool tensor = ssm_tensor(o, d_k, d_v);
+  return align_up(ssm_workspace_bytes(B * H, d_k, d_v, ssm_slots(ssm_plan(B * H, T, tensor), tensor, true)));      // (with a final state)
 }
 
 }  // namespace kata

@@ -5,6 +5,8 @@
 // memory.  Bound by fp32 issue: three operations per state entry and token.
 // Few heads: the token axis is cut into segments.  Their own states (from zero) come first, ssm_prefix turns them into the states
 // before the segments, and the second pass starts from those.
+#include <cmath>
+
 #include "kata_rows.cuh"
 #include "kata_ssm.cuh"
 
@@ -148,37 +150,39 @@ __global__ void __launch_bounds__(DV * RG) simt_ssm_kernel(const __grid_constant
   }
 }
 
-// Slot j of a head: from the own state of segment j - 1 to the state before segment j (slot 0: the state handed in).
-__global__ void __launch_bounds__(128) ssm_prefix_kernel(float* __restrict__ ws, const float* __restrict__ s_init, int BH, int segments, int se) {
+// Slot j of a head: from the own state of segment j - 1 to the state before segment j (slot 0: the state handed in).  s_final: the
+// state after the last segment, whose own state is in the slot behind.
+__global__ void __launch_bounds__(128) ssm_prefix_kernel(float* __restrict__ ws, const float* s_init, float* s_final, int BH, int segments, int slots, int se) {
   wait_for_kernels_ahead();
   constexpr int U = 8;
   const int bh = blockIdx.y, e = blockIdx.x * 128 + threadIdx.x;           // (n d_v is a multiple of 128)
-  float* s = ws + ssm_slot(segments, bh, 0) * se + e;
-  const float* decay = ws + (size_t)BH * segments * se + ssm_slot(segments, bh, 0);
+  float* s = ws + (size_t)bh * slots * se + e;
+  const float* decay = ws + (size_t)BH * slots * se + (size_t)bh * slots;
   float cur = s_init != nullptr ? s_init[(size_t)bh * se + e] : 0.f;
   s[0] = cur;
-  for (int j = 1; j < segments; j += U) {
+  for (int j = 1; j < slots; j += U) {
     float own[U], d[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (j + u < segments) {
+      if (j + u < slots) {
         own[u] = s[(size_t)(j + u) * se];
         d[u] = decay[j + u - 1];
       }
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (j + u < segments) {
+      if (j + u < slots) {
         cur = fmaf(d[u], cur, own[u]);
-        s[(size_t)(j + u) * se] = cur;
+        if (j + u < segments) s[(size_t)(j + u) * se] = cur;
       }
   }
+  if (s_final != nullptr) s_final[(size_t)bh * se + e] = cur;
 }
 
 template <typename T, int N, int DV> void launch(const Ssm& a, const SsmPlan& plan, float* ws, LaunchCtx& ctx) {
   const dim3 grid((unsigned)(a.B * a.H) * plan.segments);
   if (plan.segments > 1) {
     launch_after(ctx, simt_ssm_kernel<T, N, DV, true>, grid, dim3(DV * RG), 0, a, plan, ws);
-    ssm_prefix(a, plan, ws, ctx);
+    ssm_prefix(a, plan, plan.segments, ws, ctx);
   }
   launch_after(ctx, simt_ssm_kernel<T, N, DV, false>, grid, dim3(DV * RG), 0, a, plan, ws);
 }
@@ -198,32 +202,34 @@ template <typename T> void by_rows(const Ssm& a, const SsmPlan& plan, float* ws,
 
 }  // namespace
 
-// Segments: while the heads alone leave SMs idle, as many as fill them, of at least 256 tokens.
-SsmPlan ssm_plan(int BH, int T, int n, int d, bool tensor) {
-  const int wanted = (tensor ? 2 : 4) * kPlanSMs / BH;
-  SsmPlan p{1, T};
-  if (wanted < 2 || T < 512) return p;
-  int tokens = (T + wanted - 1) / wanted;
-  tokens = (tokens + 127) / 128 * 128;
-  p.seg_tokens = tokens < 256 ? 256 : tokens;
-  p.segments = (T + p.seg_tokens - 1) / p.seg_tokens;
-  return p;
+// Segments of whole 128-token tiles.  The second pass takes whole waves of CTAs (one per SM on the tensor cores, four of the token by
+// token kernel), the first one nearly as long again and two launches more; the number of segments with the smallest sum.
+SsmPlan ssm_plan(int BH, int T, bool tensor) {
+  const int tiles = (T + 127) / 128, resident = kPlanSMs * (tensor ? 1 : 4);
+  const double tile_us = tensor ? 0.8 : 8.0;
+  SsmPlan best{1, tiles * 128};
+  double best_us = ceil((double)BH / resident) * tiles * tile_us;
+  for (int want = 2; want <= tiles && (long long)BH * (want - 1) < 2LL * resident; ++want) {
+    const int per = (tiles + want - 1) / want, n = (tiles + per - 1) / per;
+    const double us = ceil((double)BH * n / resident) * per * tile_us * 1.8 + 8.0 + 0.1 * n;
+    if (us < best_us) {
+      best_us = us;
+      best = SsmPlan{n, per * 128};
+    }
+  }
+  return best;
 }
 
-size_t ssm_workspace_bytes(int BH, int n, int d, const SsmPlan& plan) {
-  return plan.segments > 1 ? (size_t)BH * plan.segments * ((size_t)n * d + 1) * sizeof(float) : 0;
-}
+size_t ssm_workspace_bytes(int BH, int n, int d, int slots) { return (size_t)BH * slots * ((size_t)n * d + 1) * sizeof(float); }
 
-void ssm_prefix(const Ssm& a, const SsmPlan& plan, float* ws, LaunchCtx& ctx) {
-  launch_after(ctx, ssm_prefix_kernel, dim3(a.n * a.d / 128, a.B * a.H), dim3(128), 0, ws, a.s_init, a.B * a.H, plan.segments, a.n * a.d);
+void ssm_prefix(const Ssm& a, const SsmPlan& plan, int slots, float* ws, LaunchCtx& ctx) {
+  launch_after(ctx, ssm_prefix_kernel, dim3(a.n * a.d / 128, a.B * a.H), dim3(128), 0, ws, a.s_init, slots > plan.segments ? a.s_final : nullptr, a.B * a.H,
+               plan.segments, slots, a.n * a.d);
 }
 
 void simt_ssm(const Ssm& a, const SsmPlan& plan, float* ws, LaunchCtx& ctx) {
   if (a.dtype == KATA_F32) by_rows<float>(a, plan, ws, ctx);
   else by_rows<__nv_bfloat16>(a, plan, ws, ctx);
 }
-
-bool tc_ssm_supported(int dtype, int n, int d) { return false; }
-void tc_ssm(const Ssm& a, const SsmPlan& plan, float* ws, int* device_status, LaunchCtx& ctx) {}
 
 }  // namespace kata

@@ -12,8 +12,7 @@ __device__ __forceinline__ float ssm_step_size(const Ssm& a, float dt, int h) {
   return !a.softplus || dt > 20.f ? dt : log1pf(expf(dt));
 }
 
-// Scratch of a call with several segments: the state before each of them [BH][segments][n][d] (in its place, until the prefix is
-// formed, slot j + 1 holds the own state of segment j), then the decay over each [BH][segments].
+// Place of slot j of a head in the scratch of the token by token kernel.
 __host__ __device__ inline size_t ssm_slot(int segments, int bh, int j) { return (size_t)bh * segments + j; }
 
 }  // namespace kata

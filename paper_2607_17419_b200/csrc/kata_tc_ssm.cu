@@ -1,0 +1,800 @@
+// Selective state space scan on the Blackwell tensor cores: bf16, n = 64 or 128 state rows, d_v = 64.
+//   S_t = a_t S_{t-1} + s_t k_t v_t^T,  o_t = S_t^T q_t + D v_t,  a_t = 2^(l_t), l_t = s_t A log2(e)
+// in tiles of 128 tokens, c_t the sum of l up to token t of the tile:
+//   out    O = [(Q K^T) o W + D I] V + diag(2^c) Q S,  W[t,i] = 2^(c_t - c_i) s_i for i <= t
+//   state  S <- 2^(c_127) S + K^T diag(2^(c_127 - c_i) s_i) V
+//
+// tc_ssm_out_kernel: a CTA has one head and a segment of its tokens and walks the tiles.  Scores come from the tensor cores,
+// builder warps weigh them in registers and put them back into TMEM as the bf16 A operand of the product with V.  Nothing but
+// S ties the tiles together: its fp32 entries stay in the registers of four warps, which add the tile's own state (a product of
+// its own, from V scaled and rounded to bf16) and leave a bf16 copy in shared memory for the next tile's Q S.
+// The weights of a 32 x 32 block below the diagonal are a row factor times a column factor, both at most s_i, taken at the block's
+// first row; only the four blocks on the diagonal take an exponential per entry.
+// tc_ssm_state_kernel: the segments' own states (several segments, or a final state wanted), exact to fp32: the scaled V goes in
+// as three bf16 terms (24 bits), the small ones first, and every tile's product is added in registers.
+//
+// Warps (512 threads).  Out: 0 TMA loads; 1 issues Q K^T and Q S, 2 the tile's state and the product with V; 3 decays;
+// 4-7 scaled V, state; 8-15 weights and epilogue (two warps per TMEM lane quadrant).  State: 8-15 scaled V.  All waits are bounded;
+// a warp that has TMEM to read goes on only where all its lanes saw the barrier.
+#include <cuda.h>
+
+#include "kata_rows.cuh"
+#include "kata_ssm.cuh"
+#include "kata_tmap.cuh"
+#include "kata_umma.cuh"
+
+namespace kata {
+namespace {
+
+using namespace umma;
+
+constexpr int CT = 128;                          // tokens per tile
+constexpr int DV = 64;
+constexpr int NTHREADS = 512;
+constexpr int W_STATE0 = 4, W_BLD0 = 8;
+constexpr uint32_t HALF = 16384;                 // 128 rows of 64 bf16 entries, 128B swizzle
+constexpr int NSLOT = 4;                         // tiles whose decays are held
+
+// decays of a tile
+struct Decays {
+  float rel[CT];                                 // c_t from the first token of its block of 32 (exclusive of what lies before)
+  float step[CT];                                // s_t
+  float left[CT];                                // 2^(c_127 - c_t) s_t
+  float col[192];                                // blocks 1, 2, 3: 2^(c before the block - c_i) s_i for the tokens before it
+  float before[4];                               // 2^(c before block b)
+  float total;                                   // 2^(c_127)
+  float pad[3];
+};
+
+template <int N, bool STATE> struct Shape {
+  static constexpr int HALVES = N / 64;                                        // 64-column halves of a q or k tile
+  static constexpr uint32_t K_OFF = STATE ? 0 : HALVES * HALF, V_OFF = K_OFF + HALVES * HALF;
+  static constexpr uint32_t STAGE = V_OFF + HALF;
+  static constexpr int NST = STATE ? (N == 64 ? 3 : 2) : (N == 64 ? 3 : 2);
+  static constexpr int TERMS = STATE ? 3 : 1;
+  static constexpr int XB = !STATE && N == 128 ? 1 : 2;                        // buffers of scaled V
+  static constexpr uint32_t OFF_X = NST * STAGE;
+  static constexpr uint32_t OFF_S = OFF_X + XB * TERMS * HALF;                 // [N][64] bf16
+  static constexpr uint32_t OFF_OUT = OFF_S + (STATE ? 0 : N * 128);           // 8 warps x 32 rows of 64 bytes
+  static constexpr uint32_t OFF_DEC = OFF_OUT + (STATE ? 0 : HALF);
+  static constexpr uint32_t OFF_BAR = OFF_DEC + NSLOT * sizeof(Decays);
+  static constexpr uint32_t SMEM = OFF_BAR + 512 + 1024;
+};
+static_assert(Shape<128, false>::SMEM <= 232448 && Shape<64, false>::SMEM <= 232448, "shared memory");
+static_assert(Shape<128, true>::SMEM <= 232448 && Shape<64, true>::SMEM <= 232448, "shared memory");
+static_assert(Shape<64, false>::SMEM > 116 * 1024 && Shape<64, true>::SMEM > 116 * 1024, "one CTA per SM is assumed (it takes all of TMEM)");
+
+constexpr uint32_t COL_P = 0;                    // 2 x 128: scores; the bf16 weights overwrite columns [0,32) and [64,96) of a buffer
+constexpr uint32_t COL_Y = 256, COL_R = 320;     // product with V, Q S
+constexpr uint32_t COL_SL = 384;                 // 2 x 64: own state of a tile
+constexpr uint32_t TMEM_COLS = 512;
+
+// Every barrier's phases are seen in order by all that wait for it before the next can complete (see the notes at the waits).
+enum {
+  BAR_FULL = 0,        // [3] tile landed
+  BAR_EMPTY = 3,       // [3] out: Q S and product with V done (2 commits); state: the state product done
+  BAR_DEC_FULL = 6,    // [4] decays in place (32)
+  BAR_DEC_EMPTY = 10,  // [4] decays read (one arrival per reading warp)
+  BAR_S_FULL = 14,     // [2] scores in TMEM
+  BAR_P_FULL = 16,     // [2] weights in TMEM (256)
+  BAR_P_EMPTY = 18,    // [2] weights consumed
+  BAR_O_FULL = 20,     // both products of a tile done (2 commits)
+  BAR_O_EMPTY = 21,    // results read (256)
+  BAR_X_FULL = 22,     // [2] scaled V in place (its warps' threads)
+  BAR_X_EMPTY = 24,    // [2] consumed
+  BAR_SL_FULL = 26,    // [2] own state of a tile in TMEM
+  BAR_SL_EMPTY = 28,   // [2] read (128)
+  BAR_ST = 30,         // bf16 state for the next tile in place (128)
+  BAR_R_DONE = 31,     // Q S done: the bf16 state may be overwritten
+  BAR_DRAIN = 32,
+  BAR_COUNT = 33
+};
+
+struct Args {
+  const float *A, *D, *dt_bias;
+  const void* dt;
+  long long dt0, dt1, dt2;
+  const int* lengths;
+  const float* init;           // states before the segments (slot stride) or, with one segment, before the first token; null: zero
+  float* local;                // state kernel: slots of the own states
+  float* decay;
+  __nv_bfloat16* out;
+  long long o0, o1, o2;
+  int* device_status;
+  int B, H, T, per;            // per: heads of a group
+  int segments, seg_tokens, slots;
+  bool softplus;
+  int qg, qb, kg, kb, vh, vb;  // 0 where an axis is broadcast, else 1 (coordinates of the tensor maps)
+};
+
+__device__ __forceinline__ void tma_load_4d(void* dst, const void* tmap, uint64_t* bar, int c0, int c1, int c2, int c3) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+               ::"r"(smem_u32(dst)), "l"(tmap), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
+__device__ __forceinline__ void tma_store_4d(const void* tmap, const void* src, int c0, int c1, int c2, int c3) {
+  asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4, %5}], [%1];\n\tcp.async.bulk.commit_group;"
+               ::"l"(tmap), "r"(smem_u32(src)), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
+__device__ __forceinline__ float ex2(float x) { return exp2f(x); }
+
+// The wait of a whole warp: all lanes, or none.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, wait_or_abort_counted(bar, parity, abort_flag));
+}
+
+struct Where {
+  int b, h, g, bh, seg, t0, t1, live, tiles;
+};
+__device__ __forceinline__ Where where(const Args& a) {
+  Where w;
+  w.bh = blockIdx.x / a.segments;
+  w.seg = blockIdx.x - w.bh * a.segments;
+  w.b = w.bh / a.H;
+  w.h = w.bh - w.b * a.H;
+  w.g = w.h / a.per;
+  w.t0 = w.seg * a.seg_tokens;
+  w.t1 = min(w.t0 + a.seg_tokens, a.T);
+  w.live = min(w.t1, sequence_length(a.lengths, w.b, a.T));
+  w.tiles = w.live > w.t0 ? (w.live - w.t0 + CT - 1) / CT : 0;
+  return w;
+}
+
+// Decays of the tiles, one warp: a lane has four neighbouring tokens, sums in 64 bits, the next tile's steps on their way.
+// FULL_SET: the factors of the weights too.  Returns the logarithm (base 2) of the decay over all tiles.
+template <bool FULL_SET>
+__device__ __forceinline__ double decay_warp(const Args& a, const Where& w, Decays* slots, uint64_t* bars, volatile int* abort_flag, bool& ok) {
+  const int lane = threadIdx.x & 31;
+  const __nv_bfloat16* dt = static_cast<const __nv_bfloat16*>(a.dt) + w.b * a.dt0 + w.h * a.dt1;
+  const double rate = (double)a.A[w.h] * 1.4426950408889634074;
+  const float bias = a.dt_bias != nullptr ? a.dt_bias[w.h] : 0.f;
+  double all = 0.0;
+  __nv_bfloat16 next[4];
+  auto fetch = [&](int j) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = w.t0 + j * CT + lane * 4 + i;
+      if (t < w.live) next[i] = dt[(long long)t * a.dt2];
+    }
+  };
+  if (w.tiles > 0) fetch(0);
+  for (int j = 0; j < w.tiles; ++j) {
+    float s[4];
+    double c[4], sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = w.t0 + j * CT + lane * 4 + i;
+      s[i] = 0.f;
+      if (t < w.live) {
+        const float x = __bfloat162float(next[i]) + bias;
+        s[i] = !a.softplus || x > 20.f ? x : log1pf(expf(x));
+      }
+      sum += (double)s[i] * rate;
+      c[i] = sum;
+    }
+    if (j + 1 < w.tiles) fetch(j + 1);
+    double upto = sum;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const double o = __shfl_up_sync(0xffffffffu, upto, off);
+      if (lane >= off) upto += o;
+    }
+    const double total = __shfl_sync(0xffffffffu, upto, 31);
+    const double base = upto - sum;                                // before this lane's first token
+    double ref[4];
+    ref[0] = 0.0;
+#pragma unroll
+    for (int q = 1; q < 4; ++q) ref[q] = __shfl_sync(0xffffffffu, upto, 8 * q - 1);
+    all += total;
+    const int slot = j & (NSLOT - 1);
+    ok = warp_wait(bars + BAR_DEC_EMPTY + slot, ((j / NSLOT) & 1) ^ 1, abort_flag);
+    if (!ok) break;
+    Decays& d = slots[slot];
+    float4 v;
+    v = make_float4(s[0] * ex2((float)(total - base - c[0])), s[1] * ex2((float)(total - base - c[1])), s[2] * ex2((float)(total - base - c[2])),
+                    s[3] * ex2((float)(total - base - c[3])));
+    reinterpret_cast<float4*>(d.left)[lane] = v;
+    if (lane == 0) d.total = ex2((float)total);
+    if (FULL_SET) {
+      const int blk = lane >> 3;
+      const double r = blk == 0 ? ref[0] : blk == 1 ? ref[1] : blk == 2 ? ref[2] : ref[3];
+      reinterpret_cast<float4*>(d.rel)[lane] =
+          make_float4((float)(base + c[0] - r), (float)(base + c[1] - r), (float)(base + c[2] - r), (float)(base + c[3] - r));
+      reinterpret_cast<float4*>(d.step)[lane] = make_float4(s[0], s[1], s[2], s[3]);
+#pragma unroll
+      for (int q = 1; q < 4; ++q)
+        if (blk < q)
+          reinterpret_cast<float4*>(d.col + (q == 1 ? 0 : q == 2 ? 32 : 96))[lane] =
+              make_float4(s[0] * ex2((float)(ref[q] - base - c[0])), s[1] * ex2((float)(ref[q] - base - c[1])),
+                          s[2] * ex2((float)(ref[q] - base - c[2])), s[3] * ex2((float)(ref[q] - base - c[3])));
+      if (lane < 4) d.before[lane] = ex2((float)(lane == 0 ? ref[0] : lane == 1 ? ref[1] : lane == 2 ? ref[2] : ref[3]));
+    }
+    mbar_arrive(bars + BAR_DEC_FULL + slot);
+  }
+  return all;
+}
+
+// 8 bf16 entries times a weight: bf16 terms of the products, the first rounded, the next what it left.
+template <int TERMS>
+__device__ __forceinline__ void scaled_terms(const uint4& x, float w, uint4 (&out)[TERMS]) {
+  const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+  uint32_t o[TERMS][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float lo = __uint_as_float(in[i] << 16) * w, hi = __uint_as_float(in[i] & 0xffff0000u) * w;
+#pragma unroll
+    for (int m = 0; m < TERMS; ++m) {
+      o[m][i] = pack_bf16(lo, hi);
+      if (m + 1 < TERMS) {
+        lo -= __uint_as_float(o[m][i] << 16);
+        hi -= __uint_as_float(o[m][i] & 0xffff0000u);
+      }
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < TERMS; ++m) out[m] = make_uint4(o[m][0], o[m][1], o[m][2], o[m][3]);
+}
+
+// Common start: barriers, TMEM.  Returns the aligned base of shared memory.
+__device__ __forceinline__ unsigned char* aligned_base(unsigned char* raw) {
+  return reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+}
+
+// Row of the state that a thread of the state warps holds: n = 128 all lanes, n = 64 the first 16 lanes of each warp (the lanes that a
+// product of 64 rows has).
+template <int N> __device__ __forceinline__ int state_row(int q4, int lane) { return N == 128 ? q4 * 32 + lane : q4 * 16 + lane; }
+template <int N> __device__ __forceinline__ bool state_lane(int lane) { return N == 128 || lane < 16; }
+
+template <int N>
+__global__ void __launch_bounds__(NTHREADS, 1)
+tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                  const __grid_constant__ CUtensorMap tmO, const __grid_constant__ Args a) {
+  typedef Shape<N, false> Sh;
+  constexpr int NST = Sh::NST, XB = Sh::XB, KS = N / 16;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* base = aligned_base(smem_raw);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(base + Sh::OFF_BAR);
+  Decays* decays = reinterpret_cast<Decays*>(base + Sh::OFF_DEC);
+  auto qtile = [&](int s) { return base + s * Sh::STAGE; };
+  auto ktile = [&](int s) { return base + s * Sh::STAGE + Sh::K_OFF; };
+  auto vtile = [&](int s) { return base + s * Sh::STAGE + Sh::V_OFF; };
+  auto xtile = [&](int j) { return base + Sh::OFF_X + (XB == 2 ? (j & 1) : 0) * HALF; };
+  __shared__ uint32_t tmem_base_s;
+  __shared__ int abort_s;
+  volatile int* abort_flag = &abort_s;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  bool ok = true;
+
+  if (tid == 0) {
+    abort_s = 0;
+    for (int i = 0; i < BAR_COUNT; ++i) {
+      uint32_t n = 1;
+      if (i >= BAR_EMPTY && i < BAR_EMPTY + 3) n = 2;
+      if (i >= BAR_DEC_FULL && i < BAR_DEC_FULL + NSLOT) n = 32;
+      if (i >= BAR_DEC_EMPTY && i < BAR_DEC_EMPTY + NSLOT) n = 12;
+      if (i == BAR_P_FULL || i == BAR_P_FULL + 1 || i == BAR_O_EMPTY) n = 256;
+      if (i == BAR_X_FULL || i == BAR_X_FULL + 1 || i == BAR_SL_EMPTY || i == BAR_SL_EMPTY + 1 || i == BAR_ST) n = 128;
+      if (i == BAR_O_FULL || i == BAR_DRAIN) n = 2;
+      mbar_init(bars + i, n);
+    }
+    fence_mbar_init();
+    tma_prefetch_desc(&tmQ);
+    tma_prefetch_desc(&tmK);
+    tma_prefetch_desc(&tmV);
+    tma_prefetch_desc(&tmO);
+  }
+  if (warp == 0) {
+    tmem_alloc(&tmem_base_s, TMEM_COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tb = tmem_base_s;
+  wait_for_kernels_ahead();
+  const Where w = where(a);
+
+  if (warp == 0) {
+    // =========================== TMA loads ===========================
+    if (lane == 0) {
+      for (int j = 0; j < w.tiles && ok; ++j) {
+        const int s = j % NST, tok = w.t0 + j * CT;
+        ok = wait_or_abort_counted(bars + BAR_EMPTY + s, ((j / NST) & 1) ^ 1, abort_flag);
+        if (!ok) break;
+        mbar_arrive_expect_tx(bars + BAR_FULL + s, Sh::STAGE);
+#pragma unroll
+        for (int i = 0; i < Sh::HALVES; ++i) {
+          tma_load_4d(qtile(s) + i * HALF, &tmQ, bars + BAR_FULL + s, i * 64, tok, w.g * a.qg, w.b * a.qb);
+          tma_load_4d(ktile(s) + i * HALF, &tmK, bars + BAR_FULL + s, i * 64, tok, w.g * a.kg, w.b * a.kb);
+        }
+        tma_load_4d(vtile(s), &tmV, bars + BAR_FULL + s, 0, tok, w.h * a.vh, w.b * a.vb);
+      }
+    }
+  } else if (warp == 1) {
+    // =========================== scores Q K^T, one tile ahead, and Q S ===========================
+    const uint32_t id_qk = instr_desc(kFmtBF16, kFmtBF16, 0, 0, 128, 128), id_r = instr_desc(kFmtBF16, kFmtBF16, 0, 1, 128, DV);
+    const uint64_t dk = smem_desc(0, 16, 1024, kSwizzle128B), dn = smem_desc(0, HALF, 1024, kSwizzle128B);
+    const uint32_t st = smem_u32(base + Sh::OFF_S);
+    auto scores = [&](int j) {
+      const int s = j % NST, b = j & 1;
+      if (!warp_wait(bars + BAR_FULL + s, (j / NST) & 1, abort_flag) || !warp_wait(bars + BAR_P_EMPTY + b, ((j >> 1) & 1) ^ 1, abort_flag)) return false;
+      if (elect_one()) {
+        const uint32_t qa = smem_u32(qtile(s)), ka = smem_u32(ktile(s));
+        tc_fence_after();
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+          mma_f16_ss(tb + COL_P + b * 128, at(dk, qa + (ks >> 2) * HALF + (ks & 3) * 32), at(dk, ka + (ks >> 2) * HALF + (ks & 3) * 32), id_qk, ks > 0);
+        mma_commit(bars + BAR_S_FULL + b);
+      }
+      __syncwarp();
+      return true;
+    };
+    if (w.tiles > 0) ok = scores(0);
+    for (int j = 0; j < w.tiles && ok; ++j) {
+      if (j + 1 < w.tiles) ok = scores(j + 1);
+      // the state before this tile is in place, the result of the tile before has been read
+      ok = ok && warp_wait(bars + BAR_ST, j & 1, abort_flag) && warp_wait(bars + BAR_O_EMPTY, (j & 1) ^ 1, abort_flag);
+      if (!ok) break;
+      if (elect_one()) {
+        const int s = j % NST;
+        const uint32_t qa = smem_u32(qtile(s));
+        tc_fence_after();
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+          mma_f16_ss(tb + COL_R, at(dk, qa + (ks >> 2) * HALF + (ks & 3) * 32), at(dn, st + ks * 2048), id_r, ks > 0);
+        mma_commit(bars + BAR_R_DONE);
+        mma_commit(bars + BAR_O_FULL);
+        mma_commit(bars + BAR_EMPTY + s);
+      }
+      __syncwarp();
+    }
+  } else if (warp == 2) {
+    // =========================== own state of the tile K^T V', product with V ===========================
+    const uint32_t id_s = instr_desc(kFmtBF16, kFmtBF16, 1, 1, N, DV), id_v = instr_desc(kFmtBF16, kFmtBF16, 0, 1, 128, DV);
+    const uint64_t dn = smem_desc(0, HALF, 1024, kSwizzle128B);
+    for (int j = 0; j < w.tiles && ok; ++j) {
+      const int s = j % NST, b = j & 1;
+      ok = warp_wait(bars + BAR_FULL + s, (j / NST) & 1, abort_flag) &&
+           warp_wait(bars + BAR_X_FULL + (XB == 2 ? b : 0), (XB == 2 ? j >> 1 : j) & 1, abort_flag);
+      if (ok && j + 1 < w.tiles) {
+        ok = warp_wait(bars + BAR_SL_EMPTY + b, ((j >> 1) & 1) ^ 1, abort_flag);
+        if (!ok) break;
+        if (elect_one()) {
+          const uint32_t ka = smem_u32(ktile(s)), xa = smem_u32(xtile(j));
+          tc_fence_after();
+#pragma unroll
+          for (int ks = 0; ks < CT / 16; ++ks) mma_f16_ss(tb + COL_SL + b * DV, at(dn, ka + ks * 2048), at(dn, xa + ks * 2048), id_s, ks > 0);
+          mma_commit(bars + BAR_SL_FULL + b);
+          mma_commit(bars + BAR_X_EMPTY + (XB == 2 ? b : 0));
+        }
+        __syncwarp();
+      }
+      ok = ok && warp_wait(bars + BAR_P_FULL + b, (j >> 1) & 1, abort_flag) && warp_wait(bars + BAR_O_EMPTY, (j & 1) ^ 1, abort_flag);
+      if (!ok) break;
+      if (elect_one()) {
+        const uint32_t va = smem_u32(vtile(s));
+        tc_fence_after();
+#pragma unroll
+        for (int ks = 0; ks < CT / 16; ++ks)
+          mma_f16_ts(tb + COL_Y, tb + COL_P + b * 128 + (ks >> 2) * 64 + (ks & 3) * 8, at(dn, va + ks * 2048), id_v, ks > 0);
+        mma_commit(bars + BAR_P_EMPTY + b);
+        mma_commit(bars + BAR_O_FULL);
+        mma_commit(bars + BAR_EMPTY + s);
+      }
+      __syncwarp();
+    }
+  } else if (warp == 3) {
+    // =========================== decays ===========================
+    decay_warp<true>(a, w, decays, bars, abort_flag, ok);
+  } else if (warp < W_BLD0) {
+    // =========================== scaled V, state ===========================
+    const int q4 = warp & 3, row = state_row<N>(q4, lane), tok = q4 * 32 + lane;
+    const bool mine = state_lane<N>(lane);
+    float S[DV];
+    {
+      const float* src = a.init != nullptr ? a.init + ((size_t)w.bh * a.slots + w.seg) * (N * DV) + (size_t)row * DV : nullptr;
+#pragma unroll
+      for (int c = 0; c < DV; c += 4) {
+        const float4 x = mine && src != nullptr ? *reinterpret_cast<const float4*>(src + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+        S[c] = x.x; S[c + 1] = x.y; S[c + 2] = x.z; S[c + 3] = x.w;
+      }
+    }
+    auto put_state = [&]() {                       // the bf16 copy that the next tile's Q S reads: [row][64 columns]
+      if (mine) {
+        unsigned char* dst = base + Sh::OFF_S;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          const float* x = S + 8 * c;
+          *reinterpret_cast<uint4*>(dst + sw128_offset(row, c)) =
+              make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+        }
+      }
+      fence_async_smem();
+      mbar_arrive(bars + BAR_ST);
+    };
+    // V scaled for the tile's own state (the last tile's is not needed); what lies behind the sequence's end becomes zero
+    float total = 0.f, total_next = 0.f;           // 2^(c_127) of the tile in hand and of the one ahead
+    auto put_scaled = [&](int j) {
+      const int s = j % NST, slot = j & (NSLOT - 1);
+      if (!warp_wait(bars + BAR_FULL + s, (j / NST) & 1, abort_flag) || !warp_wait(bars + BAR_DEC_FULL + slot, (j / NSLOT) & 1, abort_flag)) return false;
+      const float left = decays[slot].left[tok];
+      total_next = decays[slot].total;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bars + BAR_DEC_EMPTY + slot);
+      if (!warp_wait(bars + BAR_X_EMPTY + (XB == 2 ? (j & 1) : 0), ((XB == 2 ? j >> 1 : j) & 1) ^ 1, abort_flag)) return false;
+      const bool dead = w.t0 + j * CT + tok >= w.live;
+      if (dead) {
+        const uint4 z = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          *reinterpret_cast<uint4*>(vtile(s) + tok * 128 + c * 16) = z;
+#pragma unroll
+          for (int i = 0; i < Sh::HALVES; ++i) *reinterpret_cast<uint4*>(ktile(s) + i * HALF + tok * 128 + c * 16) = z;
+        }
+      }
+      if (j + 1 < w.tiles) {
+        unsigned char *src = vtile(s), *dst = xtile(j);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          const uint32_t off = sw128_offset(tok, c);
+          uint4 x[1];
+          scaled_terms<1>(*reinterpret_cast<const uint4*>(src + off), left, x);
+          *reinterpret_cast<uint4*>(dst + off) = x[0];
+        }
+      }
+      fence_async_smem();
+      mbar_arrive(bars + BAR_X_FULL + (XB == 2 ? (j & 1) : 0));
+      return true;
+    };
+    put_state();
+    if (w.tiles > 0) ok = put_scaled(0);
+    for (int j = 0; j < w.tiles - 1 && ok; ++j) {
+      total = total_next;
+      ok = put_scaled(j + 1);
+      if (!ok) break;
+      const int b = j & 1;
+      ok = warp_wait(bars + BAR_SL_FULL + b, (j >> 1) & 1, abort_flag);
+      if (!ok) break;
+      tc_fence_after();
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        uint32_t x[32];
+        tmem_ld32(tmem_addr(tb, q4 * 32, COL_SL + b * DV + hf * 32), x);
+        tmem_wait_ld(x);
+#pragma unroll
+        for (int c = 0; c < 32; ++c) S[hf * 32 + c] = fmaf(total, S[hf * 32 + c], __uint_as_float(x[c]));
+      }
+      tc_fence_before();
+      mbar_arrive(bars + BAR_SL_EMPTY + b);
+      ok = warp_wait(bars + BAR_R_DONE, j & 1, abort_flag);
+      if (!ok) break;
+      put_state();
+    }
+  } else {
+    // =========================== weights and epilogue (256 threads) ===========================
+    const uint32_t q4 = warp & 3;
+    const int ch = (warp - W_BLD0) >> 2;         // column half
+    const int row = q4 * 32 + lane;              // token of the tile (= TMEM lane)
+    const float skip = a.D != nullptr ? a.D[w.h] : 0.f;
+    float from_state[2] = {0.f, 0.f};            // 2^(c_t) of the tile's row, by parity of the tile
+    auto epilogue = [&](int j) {
+      if (!warp_wait(bars + BAR_O_FULL, j & 1, abort_flag)) return false;
+      tc_fence_after();
+      uint32_t y[32], r[32];
+      tmem_ld32(tmem_addr(tb, q4 * 32, COL_Y + ch * 32), y);
+      tmem_ld32(tmem_addr(tb, q4 * 32, COL_R + ch * 32), r);
+      tmem_wait_ld(y);
+      tmem_wait_ld(r);
+      tc_fence_before();
+      mbar_arrive(bars + BAR_O_EMPTY);
+      const float f = (j & 1) ? from_state[1] : from_state[0];
+      const bool dead = w.t0 + j * CT + row >= w.live;
+      unsigned char* rows = base + Sh::OFF_OUT + (warp - W_BLD0) * 2048;
+      if (lane == 0) bulk_wait_read();           // the store of the tile before has read them
+      __syncwarp();
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int e = 8 * c + 2 * i;
+          o[i] = pack_bf16(fmaf(f, __uint_as_float(r[e]), __uint_as_float(y[e])), fmaf(f, __uint_as_float(r[e + 1]), __uint_as_float(y[e + 1])));
+          if (dead) o[i] = 0u;
+        }
+        *reinterpret_cast<uint4*>(rows + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0 && w.t0 + j * CT + (int)q4 * 32 < a.T) tma_store_4d(&tmO, rows, ch * 32, w.t0 + j * CT + q4 * 32, w.h, w.b);
+      return true;
+    };
+    for (int j = 0; j < w.tiles && ok; ++j) {
+      const int b = j & 1, slot = j & (NSLOT - 1);
+      ok = warp_wait(bars + BAR_DEC_FULL + slot, (j / NSLOT) & 1, abort_flag) && warp_wait(bars + BAR_S_FULL + b, (j >> 1) & 1, abort_flag);
+      if (!ok) break;
+      tc_fence_after();
+      const Decays& d = decays[slot];
+      const float rel = d.rel[row], rf = ex2(rel);
+      if (b) from_state[1] = rf * d.before[q4];
+      else from_state[0] = rf * d.before[q4];
+      const uint32_t scol = tmem_addr(tb, q4 * 32, COL_P + b * 128 + ch * 64);
+      const float* col = d.col + (q4 < 2 ? 0 : q4 == 2 ? 32 : 96);
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        const uint32_t blk = 2 * ch + hf;        // columns 32 blk .. of the tile, against rows 32 q4 ..
+        uint32_t pk[16];
+        if (blk > q4) {
+#pragma unroll
+          for (int c = 0; c < 16; ++c) pk[c] = 0u;
+        } else {
+          uint32_t y[32];
+          tmem_ld32(scol + hf * 32, y);
+          tmem_wait_ld(y);
+          if (blk == q4) {
+#pragma unroll
+            for (int c = 0; c < 32; c += 4) {
+              const float4 rs = *reinterpret_cast<const float4*>(d.rel + blk * 32 + c), st = *reinterpret_cast<const float4*>(d.step + blk * 32 + c);
+              const float rr[4] = {rs.x, rs.y, rs.z, rs.w}, ss[4] = {st.x, st.y, st.z, st.w};
+              float v[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                v[i] = __uint_as_float(y[c + i]) * (ss[i] * ex2(rel - rr[i]));
+                if (c + i == lane) v[i] += skip;
+                if (c + i > lane) v[i] = 0.f;
+              }
+              pk[c / 2] = pack_bf16(v[0], v[1]);
+              pk[c / 2 + 1] = pack_bf16(v[2], v[3]);
+            }
+          } else {
+#pragma unroll
+            for (int c = 0; c < 32; c += 4) {
+              const float4 cf = *reinterpret_cast<const float4*>(col + blk * 32 + c);
+              pk[c / 2] = pack_bf16(__uint_as_float(y[c]) * (cf.x * rf), __uint_as_float(y[c + 1]) * (cf.y * rf));
+              pk[c / 2 + 1] = pack_bf16(__uint_as_float(y[c + 2]) * (cf.z * rf), __uint_as_float(y[c + 3]) * (cf.w * rf));
+            }
+          }
+        }
+        tmem_st16(scol + hf * 16, pk);
+      }
+      tmem_wait_st();
+      tc_fence_before();
+      mbar_arrive(bars + BAR_P_FULL + b);
+      if (lane == 0) mbar_arrive(bars + BAR_DEC_EMPTY + slot);
+      if (j > 0) ok = epilogue(j - 1);
+    }
+    if (ok && w.tiles > 0) ok = epilogue(w.tiles - 1);
+  }
+
+  // ---------------- teardown ----------------
+  if (!ok && a.device_status != nullptr) atomicExch(a.device_status, (int)KATA_ERR_DEVICE_TIMEOUT);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if ((warp == 1 || warp == 2) && lane == 0) {
+    mma_commit(bars + BAR_DRAIN);
+    mbar_wait(bars + BAR_DRAIN, 0);
+  }
+  if (warp >= W_BLD0 && lane == 0) bulk_wait();
+  __syncthreads();
+  if (warp == 0) tmem_dealloc(tb, TMEM_COLS);
+  // rows behind the last tile of the sequence
+  const int first = w.t0 + w.tiles * CT;
+  for (long long i = tid; i < (long long)(w.t1 - first) * 8; i += NTHREADS)
+    *reinterpret_cast<uint4*>(a.out + w.b * a.o0 + w.h * a.o1 + (first + (i >> 3)) * a.o2 + (i & 7) * 8) = make_uint4(0u, 0u, 0u, 0u);
+}
+
+template <int N>
+__global__ void __launch_bounds__(NTHREADS, 1)
+tc_ssm_state_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ Args a) {
+  typedef Shape<N, true> Sh;
+  constexpr int NST = Sh::NST;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* base = aligned_base(smem_raw);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(base + Sh::OFF_BAR);
+  Decays* decays = reinterpret_cast<Decays*>(base + Sh::OFF_DEC);
+  auto ktile = [&](int s) { return base + s * Sh::STAGE; };
+  auto vtile = [&](int s) { return base + s * Sh::STAGE + Sh::V_OFF; };
+  auto xtile = [&](int j, int term) { return base + Sh::OFF_X + ((j & 1) * 3 + term) * HALF; };
+  __shared__ uint32_t tmem_base_s;
+  __shared__ int abort_s;
+  volatile int* abort_flag = &abort_s;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  bool ok = true;
+  if ((int)(blockIdx.x % (unsigned)a.segments) + 2 > a.slots) return;      // (the last segment's own state is not wanted)
+
+  if (tid == 0) {
+    abort_s = 0;
+    for (int i = 0; i < BAR_COUNT; ++i) {
+      uint32_t n = 1;
+      if (i >= BAR_DEC_FULL && i < BAR_DEC_FULL + NSLOT) n = 32;
+      if (i >= BAR_DEC_EMPTY && i < BAR_DEC_EMPTY + NSLOT) n = 12;
+      if (i == BAR_X_FULL || i == BAR_X_FULL + 1) n = 256;
+      if (i == BAR_SL_EMPTY || i == BAR_SL_EMPTY + 1) n = 128;
+      mbar_init(bars + i, n);
+    }
+    fence_mbar_init();
+    tma_prefetch_desc(&tmK);
+    tma_prefetch_desc(&tmV);
+  }
+  if (warp == 0) {
+    tmem_alloc(&tmem_base_s, TMEM_COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tb = tmem_base_s;
+  wait_for_kernels_ahead();
+  const Where w = where(a);
+
+  if (warp == 0) {
+    // =========================== TMA loads ===========================
+    if (lane == 0) {
+      for (int j = 0; j < w.tiles && ok; ++j) {
+        const int s = j % NST, tok = w.t0 + j * CT;
+        ok = wait_or_abort_counted(bars + BAR_EMPTY + s, ((j / NST) & 1) ^ 1, abort_flag);
+        if (!ok) break;
+        mbar_arrive_expect_tx(bars + BAR_FULL + s, Sh::STAGE);
+#pragma unroll
+        for (int i = 0; i < Sh::HALVES; ++i) tma_load_4d(ktile(s) + i * HALF, &tmK, bars + BAR_FULL + s, i * 64, tok, w.g * a.kg, w.b * a.kb);
+        tma_load_4d(vtile(s), &tmV, bars + BAR_FULL + s, 0, tok, w.h * a.vh, w.b * a.vb);
+      }
+    }
+  } else if (warp == 1) {
+    // =========================== own state of the tile K^T V' ===========================
+    const uint32_t id_s = instr_desc(kFmtBF16, kFmtBF16, 1, 1, N, DV);
+    const uint64_t dn = smem_desc(0, HALF, 1024, kSwizzle128B);
+    for (int j = 0; j < w.tiles && ok; ++j) {
+      const int s = j % NST, b = j & 1;
+      ok = warp_wait(bars + BAR_FULL + s, (j / NST) & 1, abort_flag) && warp_wait(bars + BAR_X_FULL + b, (j >> 1) & 1, abort_flag) &&
+           warp_wait(bars + BAR_SL_EMPTY + b, ((j >> 1) & 1) ^ 1, abort_flag);
+      if (!ok) break;
+      if (elect_one()) {
+        const uint32_t ka = smem_u32(ktile(s));
+        tc_fence_after();
+#pragma unroll
+        for (int m = 2; m >= 0; --m) {           // (the small terms first)
+          const uint32_t xa = smem_u32(xtile(j, m));
+#pragma unroll
+          for (int ks = 0; ks < CT / 16; ++ks)
+            mma_f16_ss(tb + COL_SL + b * DV, at(dn, ka + ks * 2048), at(dn, xa + ks * 2048), id_s, m < 2 || ks > 0);
+        }
+        mma_commit(bars + BAR_SL_FULL + b);
+        mma_commit(bars + BAR_X_EMPTY + b);
+        mma_commit(bars + BAR_EMPTY + s);
+      }
+      __syncwarp();
+    }
+  } else if (warp == 3) {
+    // =========================== decays ===========================
+    const double all = decay_warp<false>(a, w, decays, bars, abort_flag, ok);
+    if (lane == 0) a.decay[(size_t)w.bh * a.slots + w.seg] = ex2((float)all);
+  } else if (warp >= W_STATE0 && warp < W_BLD0) {
+    // =========================== state ===========================
+    const int q4 = warp & 3, row = state_row<N>(q4, lane);
+    float S[DV];
+#pragma unroll
+    for (int c = 0; c < DV; ++c) S[c] = 0.f;
+    for (int j = 0; j < w.tiles && ok; ++j) {
+      const int b = j & 1, slot = j & (NSLOT - 1);
+      ok = warp_wait(bars + BAR_DEC_FULL + slot, (j / NSLOT) & 1, abort_flag);
+      const float total = ok ? decays[slot].total : 0.f;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bars + BAR_DEC_EMPTY + slot);
+      ok = ok && warp_wait(bars + BAR_SL_FULL + b, (j >> 1) & 1, abort_flag);
+      if (!ok) break;
+      tc_fence_after();
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        uint32_t x[32];
+        tmem_ld32(tmem_addr(tb, q4 * 32, COL_SL + b * DV + hf * 32), x);
+        tmem_wait_ld(x);
+#pragma unroll
+        for (int c = 0; c < 32; ++c) S[hf * 32 + c] = fmaf(total, S[hf * 32 + c], __uint_as_float(x[c]));
+      }
+      tc_fence_before();
+      mbar_arrive(bars + BAR_SL_EMPTY + b);
+    }
+    if (state_lane<N>(lane)) {
+      float4* dst = reinterpret_cast<float4*>(a.local + ((size_t)w.bh * a.slots + w.seg + 1) * (N * DV) + (size_t)row * DV);
+#pragma unroll
+      for (int c = 0; c < DV / 4; ++c) dst[c] = make_float4(S[4 * c], S[4 * c + 1], S[4 * c + 2], S[4 * c + 3]);
+    }
+  } else if (warp >= W_BLD0) {
+    // =========================== scaled V in three terms ===========================
+    const int q4 = warp & 3, ch = (warp - W_BLD0) >> 2, tok = q4 * 32 + lane;
+    for (int j = 0; j < w.tiles && ok; ++j) {
+      const int s = j % NST, b = j & 1, slot = j & (NSLOT - 1);
+      ok = warp_wait(bars + BAR_DEC_FULL + slot, (j / NSLOT) & 1, abort_flag);
+      const float left = ok ? decays[slot].left[tok] : 0.f;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bars + BAR_DEC_EMPTY + slot);
+      ok = ok && warp_wait(bars + BAR_FULL + s, (j / NST) & 1, abort_flag) && warp_wait(bars + BAR_X_EMPTY + b, ((j >> 1) & 1) ^ 1, abort_flag);
+      if (!ok) break;
+      const bool dead = w.t0 + j * CT + tok >= w.live;
+#pragma unroll
+      for (int c = 4 * ch; c < 4 * ch + 4; ++c) {
+        const uint32_t off = sw128_offset(tok, c);
+        uint4 v = *reinterpret_cast<const uint4*>(vtile(s) + off), x[3];
+        if (dead) {                              // (K times zero has to be zero, whatever lies there)
+          v = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+          for (int i = 0; i < Sh::HALVES; ++i) *reinterpret_cast<uint4*>(ktile(s) + i * HALF + off) = v;
+        }
+        scaled_terms<3>(v, left, x);
+#pragma unroll
+        for (int m = 0; m < 3; ++m) *reinterpret_cast<uint4*>(xtile(j, m) + off) = x[m];
+      }
+      fence_async_smem();
+      mbar_arrive(bars + BAR_X_FULL + b);
+    }
+  }
+
+  // ---------------- teardown ----------------
+  if (!ok && a.device_status != nullptr) atomicExch(a.device_status, (int)KATA_ERR_DEVICE_TIMEOUT);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 1 && lane == 0) {
+    mma_commit(bars + BAR_DRAIN);
+    mbar_wait(bars + BAR_DRAIN, 0);
+  }
+  __syncthreads();
+  if (warp == 0) tmem_dealloc(tb, TMEM_COLS);
+}
+
+// [B][heads][T][width] bf16 view, box = cols x rows x 1 x 1; axes that are broadcast (stride 0) have one entry and a coordinate of 0.
+bool make_view_map(CUtensorMap* tm, const View& v, int B, int heads, int T, int width, int cols, int rows, int* head_on, int* batch_on) {
+  EncodeTiledFn fn = tensor_map_encoder();
+  if (fn == nullptr) return false;
+  *head_on = v.s1 != 0;
+  *batch_on = v.s0 != 0;
+  const cuuint64_t dims[4] = {(cuuint64_t)width, (cuuint64_t)T, (cuuint64_t)(v.s1 != 0 ? heads : 1), (cuuint64_t)(v.s0 != 0 ? B : 1)};
+  const cuuint64_t strides[3] = {(cuuint64_t)(T > 1 ? v.s2 * 2 : 16), (cuuint64_t)(v.s1 != 0 ? v.s1 * 2 : 16), (cuuint64_t)(v.s0 != 0 ? v.s0 * 2 : 16)};
+  const cuuint32_t box[4] = {(cuuint32_t)cols, (cuuint32_t)rows, 1, 1}, es[4] = {1, 1, 1, 1};
+  return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, v.p, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int N> void launch(const Ssm& a, const SsmPlan& plan, float* ws, int* device_status, LaunchCtx& ctx) {
+  CUtensorMap tmQ, tmK, tmV, tmO;
+  Args r = {};
+  int on[2];
+  if (!make_view_map(&tmQ, a.q, a.B, a.G, a.T, N, 64, CT, &r.qg, &r.qb) || !make_view_map(&tmK, a.k, a.B, a.G, a.T, N, 64, CT, &r.kg, &r.kb) ||
+      !make_view_map(&tmV, a.v, a.B, a.H, a.T, DV, 64, CT, &r.vh, &r.vb) || !make_view_map(&tmO, a.out, a.B, a.H, a.T, DV, 32, 32, &on[0], &on[1]) ||
+      !allow_smem<tc_ssm_out_kernel<N>>((int)Shape<N, false>::SMEM) || !allow_smem<tc_ssm_state_kernel<N>>((int)Shape<N, true>::SMEM)) {
+    ctx.status = KATA_ERR_CUDA;
+    return;
+  }
+  r.A = a.A; r.D = a.D; r.dt_bias = a.dt_bias;
+  r.dt = a.dt.p; r.dt0 = a.dt.s0; r.dt1 = a.dt.s1; r.dt2 = a.dt.s2;
+  r.lengths = a.lengths;
+  r.out = reinterpret_cast<__nv_bfloat16*>(a.out.p); r.o0 = a.out.s0; r.o1 = a.out.s1; r.o2 = a.out.s2;
+  r.device_status = device_status;
+  r.B = a.B; r.H = a.H; r.T = a.T; r.per = a.H / a.G;
+  r.segments = plan.segments; r.seg_tokens = plan.seg_tokens;
+  r.softplus = a.softplus;
+  const dim3 grid((unsigned)(a.B * a.H) * plan.segments);
+  const bool states = plan.segments > 1 || a.s_final != nullptr;
+  r.slots = states ? plan.segments + (a.s_final != nullptr ? 1 : 0) : 1;
+  r.init = a.s_init;
+  if (states) {
+    r.local = ws;
+    r.decay = ws + (size_t)a.B * a.H * r.slots * (N * DV);
+    launch_after(ctx, tc_ssm_state_kernel<N>, grid, dim3(NTHREADS), Shape<N, true>::SMEM, tmK, tmV, r);
+    ssm_prefix(a, plan, r.slots, ws, ctx);
+    r.init = ws;
+  }
+  launch_after(ctx, tc_ssm_out_kernel<N>, grid, dim3(NTHREADS), Shape<N, false>::SMEM, tmQ, tmK, tmV, tmO, r);
+}
+
+}  // namespace
+
+bool tc_ssm_supported(int dtype, int n, int d) { return dtype == KATA_BF16 && (n == 64 || n == 128) && d == DV; }
+
+void tc_ssm(const Ssm& a, const SsmPlan& plan, float* ws, int* device_status, LaunchCtx& ctx) {
+  if (a.n == 64) launch<64>(a, plan, ws, device_status, ctx);
+  else launch<128>(a, plan, ws, device_status, ctx);
+}
+
+}  // namespace kata

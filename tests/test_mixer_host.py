@@ -172,7 +172,9 @@ def test_ssm_arguments(L, fn):
 def test_workspace_of_bad_sizes_is_zero(L):
     ws = kb.kata_workspace_bytes
     assert ws(kb.KATA_FN_SSM_SCAN, 1, 2, 9000, 48, 64, 0, opts()) == 0 and ws(kb.KATA_FN_SSM_SCAN, 0, 2, 9000, 64, 64, 0, opts()) == 0
-    assert ws(kb.KATA_FN_SSM_SCAN, 64, 16, 4096, 64, 64, 0, opts()) == 0           # heads enough: one segment
+    up = lambda n: (n + 255) // 256 * 256
+    assert ws(kb.KATA_FN_SSM_SCAN, 64, 16, 4096, 64, 32, 0, opts()) == 0           # heads enough: one segment
+    assert ws(kb.KATA_FN_SSM_SCAN, 64, 16, 4096, 64, 64, 0, opts()) == up(64 * 16 * 2 * (64 * 64 + 1) * 4)   # (with a final state)
     assert ws(kb.KATA_FN_BWD_SHORT_CONV, 1, 64, 100, 7, 0, 0, opts()) == 0 and ws(kb.KATA_FN_BWD_NORM_ROPE, 1, 4, 100, 48, 0, 0, opts()) == 0
     assert ws(kb.KATA_FN_SSM_SCAN | kb.KATA_FN_HOST_IO, 1, 2, 9000, 64, 64, 0, opts()) == 0
 
