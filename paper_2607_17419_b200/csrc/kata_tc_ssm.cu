@@ -1,21 +1,24 @@
 // Selective state space scan on the Blackwell tensor cores: bf16, n = 64 or 128 state rows, d_v = 64.
 //   S_t = a_t S_{t-1} + s_t k_t v_t^T,  o_t = S_t^T q_t + D v_t,  a_t = 2^(l_t), l_t = s_t A log2(e)
 // in tiles of 128 tokens, c_t the sum of l up to token t of the tile:
-//   out    O = [(Q K^T) o W + D I] V + diag(2^c) Q S,  W[t,i] = 2^(c_t - c_i) s_i for i <= t
+//   out    O = [(Q K^T) o W] V + diag(2^c) Q S + D V,  W[t,i] = 2^(c_t - c_i) s_i for i <= t
 //   state  S <- 2^(c_127) S + K^T diag(2^(c_127 - c_i) s_i) V
 //
 // tc_ssm_out_kernel: a CTA has one head and a segment of its tokens and walks the tiles.  Scores come from the tensor cores,
 // builder warps weigh them in registers and put them back into TMEM as the bf16 A operand of the product with V.  Nothing but
 // S ties the tiles together: its fp32 entries stay in the registers of four warps, which add the tile's own state (a product of
 // its own, from V scaled and rounded to bf16) and leave a bf16 copy in shared memory for the next tile's Q S.
-// The weights of a 32 x 32 block below the diagonal are a row factor times a column factor, both at most s_i, taken at the block's
-// first row; only the four blocks on the diagonal take an exponential per entry.
+// The weights of a 32 x 32 block are a row factor times a column factor, taken at the start of the rows' block: below the diagonal
+// both are at most s_i, on the diagonal the column factor is 2^(-c_i) s_i, and blocks that decay by more than 2^-100 in their 32
+// tokens take an exponential per entry instead.  So a tile takes a few exponentials per token and two products per score.
 // tc_ssm_state_kernel: the segments' own states (several segments, or a final state wanted), exact to fp32: the scaled V goes in
 // as three bf16 terms (24 bits), the small ones first, and every tile's product is added in registers.
 //
-// Warps (512 threads).  Out: 0 TMA loads; 1 issues Q K^T and Q S, 2 the tile's state and the product with V; 3 decays;
-// 4-7 scaled V, state; 8-15 weights and epilogue (two warps per TMEM lane quadrant).  State: 8-15 scaled V.  All waits are bounded;
-// a warp that has TMEM to read goes on only where all its lanes saw the barrier.
+// Warps (512 threads).  Out: 0 decays; 1 issues Q K^T and Q S, 2 the tile's state and the product with V; 3 TMA loads;
+// 4-7 scaled V, state; 8-15 weights and epilogue (two warps per TMEM lane quadrant).  State: 8-15 scaled V.  The roles' loops are
+// written once each and kept short: sixteen warps in unlike code of some thousand instructions each waited for instructions most of
+// the time (8 x 16 heads x 4096 tokens 135 us).  All waits are bounded; a warp that has TMEM to read goes on only where all its
+// lanes saw the barrier.
 #include <cuda.h>
 
 #include "kata_rows.cuh"
@@ -35,15 +38,18 @@ constexpr int W_STATE0 = 4, W_BLD0 = 8;
 constexpr uint32_t HALF = 16384;                 // 128 rows of 64 bf16 entries, 128B swizzle
 constexpr int NSLOT = 4;                         // tiles whose decays are held
 
-// decays of a tile
+// Decays of a tile, c_t counted from the start of the token's block of 32.
 struct Decays {
-  float rel[CT];                                 // c_t from the first token of its block of 32 (exclusive of what lies before)
-  float step[CT];                                // s_t
-  float left[CT];                                // 2^(c_127 - c_t) s_t
-  float col[192];                                // blocks 1, 2, 3: 2^(c before the block - c_i) s_i for the tokens before it
-  float before[4];                               // 2^(c before block b)
-  float total;                                   // 2^(c_127)
-  float pad[3];
+  float row[CT];                                 // 2^(c_t)
+  float tail[CT];                                // 2^(c at the end of the block - c_t) s_t
+  float inv[CT];                                 // 2^(-c_t) s_t
+  float left[CT];                                // 2^(c at the end of the tile - c_t) s_t
+  float rel[CT], step[CT];                       // c_t, s_t
+  float before[4];                               // 2^(c from the start of the tile to block b)
+  float between[4][4];                           // [r][b]: 2^(c from the end of block b to the start of block r), b < r
+  float total;                                   // 2^(c of the whole tile)
+  int steep;                                     // bit b: block b decays (or grows) by more than 2^100
+  float pad[2];
 };
 
 template <int N, bool STATE> struct Shape {
@@ -72,7 +78,7 @@ constexpr uint32_t TMEM_COLS = 512;
 // Every barrier's phases are seen in order by all that wait for it before the next can complete (see the notes at the waits).
 enum {
   BAR_FULL = 0,        // [3] tile landed
-  BAR_EMPTY = 3,       // [3] out: Q S and product with V done (2 commits); state: the state product done
+  BAR_EMPTY = 3,       // [3] out: Q S and product with V done (2 commits), V read (8 warps); state: the state product done
   BAR_DEC_FULL = 6,    // [4] decays in place (32)
   BAR_DEC_EMPTY = 10,  // [4] decays read (one arrival per reading warp)
   BAR_S_FULL = 14,     // [2] scores in TMEM
@@ -115,7 +121,28 @@ __device__ __forceinline__ void tma_store_4d(const void* tmap, const void* src, 
   asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4, %5}], [%1];\n\tcp.async.bulk.commit_group;"
                ::"l"(tmap), "r"(smem_u32(src)), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
 }
-__device__ __forceinline__ float ex2(float x) { return exp2f(x); }
+// 2^x to 2^-22 (what is below 2^-126 is zero)
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 c;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(*reinterpret_cast<unsigned long long*>(&c))
+      : "l"(*reinterpret_cast<const unsigned long long*>(&a)), "l"(*reinterpret_cast<const unsigned long long*>(&b)));
+  return c;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(*reinterpret_cast<unsigned long long*>(&d))
+      : "l"(*reinterpret_cast<const unsigned long long*>(&a)), "l"(*reinterpret_cast<const unsigned long long*>(&b)),
+        "l"(*reinterpret_cast<const unsigned long long*>(&c)));
+  return d;
+}
+__device__ __forceinline__ float2 f2(uint32_t lo, uint32_t hi) { return make_float2(__uint_as_float(lo), __uint_as_float(hi)); }
+__device__ __forceinline__ float2 unpack(uint32_t x) { return f2(x << 16, x & 0xffff0000u); }
 
 // The wait of a whole warp: all lanes, or none.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
@@ -139,74 +166,74 @@ __device__ __forceinline__ Where where(const Args& a) {
   return w;
 }
 
-// Decays of the tiles, one warp: a lane has four neighbouring tokens, sums in 64 bits, the next tile's steps on their way.
-// FULL_SET: the factors of the weights too.  Returns the logarithm (base 2) of the decay over all tiles.
-template <bool FULL_SET>
+// Decays of the tiles, one warp: a lane has four neighbouring tokens, eight lanes a block; the next tile's steps are on their way.
+// ALL: the factors of the weights too.  Returns the logarithm (base 2) of the decay over all tiles.
+template <bool ALL>
 __device__ __forceinline__ double decay_warp(const Args& a, const Where& w, Decays* slots, uint64_t* bars, volatile int* abort_flag, bool& ok) {
   const int lane = threadIdx.x & 31;
   const __nv_bfloat16* dt = static_cast<const __nv_bfloat16*>(a.dt) + w.b * a.dt0 + w.h * a.dt1;
-  const double rate = (double)a.A[w.h] * 1.4426950408889634074;
+  const float rate = (float)((double)a.A[w.h] * 1.4426950408889634074);
   const float bias = a.dt_bias != nullptr ? a.dt_bias[w.h] : 0.f;
   double all = 0.0;
-  __nv_bfloat16 next[4];
+  float next[4];
   auto fetch = [&](int j) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int t = w.t0 + j * CT + lane * 4 + i;
-      if (t < w.live) next[i] = dt[(long long)t * a.dt2];
+      next[i] = t < w.live ? __bfloat162float(dt[(long long)t * a.dt2]) + bias : 0.f;
     }
   };
   if (w.tiles > 0) fetch(0);
+#pragma unroll 1
   for (int j = 0; j < w.tiles; ++j) {
-    float s[4];
-    double c[4], sum = 0.0;
+    float s[4], c[4], sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int t = w.t0 + j * CT + lane * 4 + i;
-      s[i] = 0.f;
-      if (t < w.live) {
-        const float x = __bfloat162float(next[i]) + bias;
-        s[i] = !a.softplus || x > 20.f ? x : log1pf(expf(x));
-      }
-      sum += (double)s[i] * rate;
+      s[i] = !a.softplus || next[i] > 20.f ? next[i] : log1pf(expf(next[i]));
+      if (w.t0 + j * CT + lane * 4 + i >= w.live) s[i] = 0.f;
+      sum = fmaf(s[i], rate, sum);
       c[i] = sum;
     }
     if (j + 1 < w.tiles) fetch(j + 1);
-    double upto = sum;
+    float upto = sum;                            // from the start of the block
 #pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const double o = __shfl_up_sync(0xffffffffu, upto, off);
-      if (lane >= off) upto += o;
+    for (int off = 1; off < 8; off <<= 1) {
+      const float o = __shfl_up_sync(0xffffffffu, upto, off, 8);
+      if ((lane & 7) >= off) upto += o;
     }
-    const double total = __shfl_sync(0xffffffffu, upto, 31);
-    const double base = upto - sum;                                // before this lane's first token
-    double ref[4];
-    ref[0] = 0.0;
-#pragma unroll
-    for (int q = 1; q < 4; ++q) ref[q] = __shfl_sync(0xffffffffu, upto, 8 * q - 1);
-    all += total;
-    const int slot = j & (NSLOT - 1);
+    const float base = upto - sum, mine = __shfl_sync(0xffffffffu, upto, 7, 8);     // before this lane's tokens; of the whole block
+    const float b0 = __shfl_sync(0xffffffffu, mine, 0), b1 = __shfl_sync(0xffffffffu, mine, 8), b2 = __shfl_sync(0xffffffffu, mine, 16),
+                b3 = __shfl_sync(0xffffffffu, mine, 24);
+    all += (double)b0 + b1 + b2 + b3;
+    const int blk = lane >> 3, slot = j & (NSLOT - 1);
+    const float behind = ex2(blk == 0 ? b1 + b2 + b3 : blk == 1 ? b2 + b3 : blk == 2 ? b3 : 0.f);
     ok = warp_wait(bars + BAR_DEC_EMPTY + slot, ((j / NSLOT) & 1) ^ 1, abort_flag);
     if (!ok) break;
     Decays& d = slots[slot];
-    float4 v;
-    v = make_float4(s[0] * ex2((float)(total - base - c[0])), s[1] * ex2((float)(total - base - c[1])), s[2] * ex2((float)(total - base - c[2])),
-                    s[3] * ex2((float)(total - base - c[3])));
-    reinterpret_cast<float4*>(d.left)[lane] = v;
-    if (lane == 0) d.total = ex2((float)total);
-    if (FULL_SET) {
-      const int blk = lane >> 3;
-      const double r = blk == 0 ? ref[0] : blk == 1 ? ref[1] : blk == 2 ? ref[2] : ref[3];
-      reinterpret_cast<float4*>(d.rel)[lane] =
-          make_float4((float)(base + c[0] - r), (float)(base + c[1] - r), (float)(base + c[2] - r), (float)(base + c[3] - r));
-      reinterpret_cast<float4*>(d.step)[lane] = make_float4(s[0], s[1], s[2], s[3]);
+    float tail[4];
 #pragma unroll
-      for (int q = 1; q < 4; ++q)
-        if (blk < q)
-          reinterpret_cast<float4*>(d.col + (q == 1 ? 0 : q == 2 ? 32 : 96))[lane] =
-              make_float4(s[0] * ex2((float)(ref[q] - base - c[0])), s[1] * ex2((float)(ref[q] - base - c[1])),
-                          s[2] * ex2((float)(ref[q] - base - c[2])), s[3] * ex2((float)(ref[q] - base - c[3])));
-      if (lane < 4) d.before[lane] = ex2((float)(lane == 0 ? ref[0] : lane == 1 ? ref[1] : lane == 2 ? ref[2] : ref[3]));
+    for (int i = 0; i < 4; ++i) {
+      c[i] += base;
+      tail[i] = s[i] * ex2(mine - c[i]);
+    }
+    reinterpret_cast<float4*>(d.left)[lane] = make_float4(tail[0] * behind, tail[1] * behind, tail[2] * behind, tail[3] * behind);
+    if (ALL) {
+      reinterpret_cast<float4*>(d.tail)[lane] = make_float4(tail[0], tail[1], tail[2], tail[3]);
+      reinterpret_cast<float4*>(d.row)[lane] = make_float4(ex2(c[0]), ex2(c[1]), ex2(c[2]), ex2(c[3]));
+      reinterpret_cast<float4*>(d.inv)[lane] = make_float4(s[0] * ex2(-c[0]), s[1] * ex2(-c[1]), s[2] * ex2(-c[2]), s[3] * ex2(-c[3]));
+      reinterpret_cast<float4*>(d.rel)[lane] = make_float4(c[0], c[1], c[2], c[3]);
+      reinterpret_cast<float4*>(d.step)[lane] = make_float4(s[0], s[1], s[2], s[3]);
+      const unsigned steep = __ballot_sync(0xffffffffu, !(fabsf(c[0]) < 100.f && fabsf(c[1]) < 100.f && fabsf(c[2]) < 100.f && fabsf(c[3]) < 100.f));
+      // lanes 0-3: before; 4: the whole tile; 5: [2][0], 6: [3][0], 7: [3][1]; neighbours are 1
+      const float e = ex2(lane == 1 ? b0 : lane == 2 ? b0 + b1 : lane == 3 ? b0 + b1 + b2 : lane == 4 ? (b0 + b1) + (b2 + b3) : lane == 5 ? b1
+                          : lane == 6 ? b1 + b2 : lane == 7 ? b2 : 0.f);
+      if (lane < 4) d.before[lane] = e;
+      if (lane == 4) d.total = e;
+      if (lane >= 5 && lane < 8) d.between[lane == 5 ? 2 : 3][lane == 7 ? 1 : 0] = e;
+      if (lane >= 8 && lane < 11) d.between[lane - 7][lane - 8] = 1.f;
+      if (lane == 11) d.steep = ((steep & 0xffu) != 0 ? 1 : 0) | ((steep & 0xff00u) != 0 ? 2 : 0) | ((steep & 0xff0000u) != 0 ? 4 : 0) | ((steep >> 24) != 0 ? 8 : 0);
+    } else if (lane == 0) {
+      d.total = ex2((b0 + b1) + (b2 + b3));
     }
     mbar_arrive(bars + BAR_DEC_FULL + slot);
   }
@@ -220,14 +247,11 @@ __device__ __forceinline__ void scaled_terms(const uint4& x, float w, uint4 (&ou
   uint32_t o[TERMS][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    float lo = __uint_as_float(in[i] << 16) * w, hi = __uint_as_float(in[i] & 0xffff0000u) * w;
+    float2 p = mul2(unpack(in[i]), make_float2(w, w));
 #pragma unroll
     for (int m = 0; m < TERMS; ++m) {
-      o[m][i] = pack_bf16(lo, hi);
-      if (m + 1 < TERMS) {
-        lo -= __uint_as_float(o[m][i] << 16);
-        hi -= __uint_as_float(o[m][i] & 0xffff0000u);
-      }
+      o[m][i] = pack_bf16(p.x, p.y);
+      if (m + 1 < TERMS) p = fma2(unpack(o[m][i]), make_float2(-1.f, -1.f), p);
     }
   }
 #pragma unroll
@@ -268,7 +292,7 @@ tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     abort_s = 0;
     for (int i = 0; i < BAR_COUNT; ++i) {
       uint32_t n = 1;
-      if (i >= BAR_EMPTY && i < BAR_EMPTY + 3) n = 2;
+      if (i >= BAR_EMPTY && i < BAR_EMPTY + 3) n = 2 + 8;
       if (i >= BAR_DEC_FULL && i < BAR_DEC_FULL + NSLOT) n = 32;
       if (i >= BAR_DEC_EMPTY && i < BAR_DEC_EMPTY + NSLOT) n = 12;
       if (i == BAR_P_FULL || i == BAR_P_FULL + 1 || i == BAR_O_EMPTY) n = 256;
@@ -294,66 +318,61 @@ tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   const Where w = where(a);
 
   if (warp == 0) {
-    // =========================== TMA loads ===========================
-    if (lane == 0) {
-      for (int j = 0; j < w.tiles && ok; ++j) {
-        const int s = j % NST, tok = w.t0 + j * CT;
-        ok = wait_or_abort_counted(bars + BAR_EMPTY + s, ((j / NST) & 1) ^ 1, abort_flag);
-        if (!ok) break;
-        mbar_arrive_expect_tx(bars + BAR_FULL + s, Sh::STAGE);
-#pragma unroll
-        for (int i = 0; i < Sh::HALVES; ++i) {
-          tma_load_4d(qtile(s) + i * HALF, &tmQ, bars + BAR_FULL + s, i * 64, tok, w.g * a.qg, w.b * a.qb);
-          tma_load_4d(ktile(s) + i * HALF, &tmK, bars + BAR_FULL + s, i * 64, tok, w.g * a.kg, w.b * a.kb);
-        }
-        tma_load_4d(vtile(s), &tmV, bars + BAR_FULL + s, 0, tok, w.h * a.vh, w.b * a.vb);
-      }
-    }
+    // =========================== decays ===========================
+    decay_warp<true>(a, w, decays, bars, abort_flag, ok);
   } else if (warp == 1) {
     // =========================== scores Q K^T, one tile ahead, and Q S ===========================
     const uint32_t id_qk = instr_desc(kFmtBF16, kFmtBF16, 0, 0, 128, 128), id_r = instr_desc(kFmtBF16, kFmtBF16, 0, 1, 128, DV);
     const uint64_t dk = smem_desc(0, 16, 1024, kSwizzle128B), dn = smem_desc(0, HALF, 1024, kSwizzle128B);
     const uint32_t st = smem_u32(base + Sh::OFF_S);
-    auto scores = [&](int j) {
-      const int s = j % NST, b = j & 1;
-      if (!warp_wait(bars + BAR_FULL + s, (j / NST) & 1, abort_flag) || !warp_wait(bars + BAR_P_EMPTY + b, ((j >> 1) & 1) ^ 1, abort_flag)) return false;
-      if (elect_one()) {
-        const uint32_t qa = smem_u32(qtile(s)), ka = smem_u32(ktile(s));
-        tc_fence_after();
+    int s = 0, s_before = 0, round = 0;
+#pragma unroll 1
+    for (int j = 0; j <= w.tiles && ok; ++j) {
+      if (j < w.tiles) {
+        const int b = j & 1;
+        ok = warp_wait(bars + BAR_FULL + s, round & 1, abort_flag) && warp_wait(bars + BAR_P_EMPTY + b, ((j >> 1) & 1) ^ 1, abort_flag);
+        if (!ok) break;
+        if (elect_one()) {
+          const uint32_t qa = smem_u32(qtile(s)), ka = smem_u32(ktile(s));
+          tc_fence_after();
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-          mma_f16_ss(tb + COL_P + b * 128, at(dk, qa + (ks >> 2) * HALF + (ks & 3) * 32), at(dk, ka + (ks >> 2) * HALF + (ks & 3) * 32), id_qk, ks > 0);
-        mma_commit(bars + BAR_S_FULL + b);
+          for (int ks = 0; ks < KS; ++ks)
+            mma_f16_ss(tb + COL_P + b * 128, at(dk, qa + (ks >> 2) * HALF + (ks & 3) * 32), at(dk, ka + (ks >> 2) * HALF + (ks & 3) * 32), id_qk, ks > 0);
+          mma_commit(bars + BAR_S_FULL + b);
+        }
+        __syncwarp();
       }
-      __syncwarp();
-      return true;
-    };
-    if (w.tiles > 0) ok = scores(0);
-    for (int j = 0; j < w.tiles && ok; ++j) {
-      if (j + 1 < w.tiles) ok = scores(j + 1);
-      // the state before this tile is in place, the result of the tile before has been read
-      ok = ok && warp_wait(bars + BAR_ST, j & 1, abort_flag) && warp_wait(bars + BAR_O_EMPTY, (j & 1) ^ 1, abort_flag);
-      if (!ok) break;
-      if (elect_one()) {
-        const int s = j % NST;
-        const uint32_t qa = smem_u32(qtile(s));
-        tc_fence_after();
+      if (j > 0) {
+        // the state before the tile is in place, the result of the tile before it has been read
+        ok = warp_wait(bars + BAR_ST, (j - 1) & 1, abort_flag) && warp_wait(bars + BAR_O_EMPTY, j & 1, abort_flag);
+        if (!ok) break;
+        if (elect_one()) {
+          const uint32_t qa = smem_u32(qtile(s_before));
+          tc_fence_after();
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-          mma_f16_ss(tb + COL_R, at(dk, qa + (ks >> 2) * HALF + (ks & 3) * 32), at(dn, st + ks * 2048), id_r, ks > 0);
-        mma_commit(bars + BAR_R_DONE);
-        mma_commit(bars + BAR_O_FULL);
-        mma_commit(bars + BAR_EMPTY + s);
+          for (int ks = 0; ks < KS; ++ks)
+            mma_f16_ss(tb + COL_R, at(dk, qa + (ks >> 2) * HALF + (ks & 3) * 32), at(dn, st + ks * 2048), id_r, ks > 0);
+          mma_commit(bars + BAR_R_DONE);
+          mma_commit(bars + BAR_O_FULL);
+          mma_commit(bars + BAR_EMPTY + s_before);
+        }
+        __syncwarp();
       }
-      __syncwarp();
+      s_before = s;
+      if (++s == NST) {
+        s = 0;
+        ++round;
+      }
     }
   } else if (warp == 2) {
     // =========================== own state of the tile K^T V', product with V ===========================
     const uint32_t id_s = instr_desc(kFmtBF16, kFmtBF16, 1, 1, N, DV), id_v = instr_desc(kFmtBF16, kFmtBF16, 0, 1, 128, DV);
     const uint64_t dn = smem_desc(0, HALF, 1024, kSwizzle128B);
+    int s = 0, round = 0;
+#pragma unroll 1
     for (int j = 0; j < w.tiles && ok; ++j) {
-      const int s = j % NST, b = j & 1;
-      ok = warp_wait(bars + BAR_FULL + s, (j / NST) & 1, abort_flag) &&
+      const int b = j & 1;
+      ok = warp_wait(bars + BAR_FULL + s, round & 1, abort_flag) &&
            warp_wait(bars + BAR_X_FULL + (XB == 2 ? b : 0), (XB == 2 ? j >> 1 : j) & 1, abort_flag);
       if (ok && j + 1 < w.tiles) {
         ok = warp_wait(bars + BAR_SL_EMPTY + b, ((j >> 1) & 1) ^ 1, abort_flag);
@@ -381,59 +400,66 @@ tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         mma_commit(bars + BAR_EMPTY + s);
       }
       __syncwarp();
+      if (++s == NST) {
+        s = 0;
+        ++round;
+      }
     }
   } else if (warp == 3) {
-    // =========================== decays ===========================
-    decay_warp<true>(a, w, decays, bars, abort_flag, ok);
+    // =========================== TMA loads ===========================
+    if (lane == 0) {
+      for (int j = 0; j < w.tiles && ok; ++j) {
+        const int s = j % NST, tok = w.t0 + j * CT;
+        ok = wait_or_abort_counted(bars + BAR_EMPTY + s, ((j / NST) & 1) ^ 1, abort_flag);
+        if (!ok) break;
+        mbar_arrive_expect_tx(bars + BAR_FULL + s, Sh::STAGE);
+#pragma unroll
+        for (int i = 0; i < Sh::HALVES; ++i) {
+          tma_load_4d(qtile(s) + i * HALF, &tmQ, bars + BAR_FULL + s, i * 64, tok, w.g * a.qg, w.b * a.qb);
+          tma_load_4d(ktile(s) + i * HALF, &tmK, bars + BAR_FULL + s, i * 64, tok, w.g * a.kg, w.b * a.kb);
+        }
+        tma_load_4d(vtile(s), &tmV, bars + BAR_FULL + s, 0, tok, w.h * a.vh, w.b * a.vb);
+      }
+    }
   } else if (warp < W_BLD0) {
     // =========================== scaled V, state ===========================
     const int q4 = warp & 3, row = state_row<N>(q4, lane), tok = q4 * 32 + lane;
     const bool mine = state_lane<N>(lane);
-    float S[DV];
+    float2 S[DV / 2];
     {
       const float* src = a.init != nullptr ? a.init + ((size_t)w.bh * a.slots + w.seg) * (N * DV) + (size_t)row * DV : nullptr;
 #pragma unroll
       for (int c = 0; c < DV; c += 4) {
         const float4 x = mine && src != nullptr ? *reinterpret_cast<const float4*>(src + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-        S[c] = x.x; S[c + 1] = x.y; S[c + 2] = x.z; S[c + 3] = x.w;
+        S[c / 2] = make_float2(x.x, x.y);
+        S[c / 2 + 1] = make_float2(x.z, x.w);
       }
     }
-    auto put_state = [&]() {                       // the bf16 copy that the next tile's Q S reads: [row][64 columns]
-      if (mine) {
-        unsigned char* dst = base + Sh::OFF_S;
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          const float* x = S + 8 * c;
-          *reinterpret_cast<uint4*>(dst + sw128_offset(row, c)) =
-              make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-        }
-      }
-      fence_async_smem();
-      mbar_arrive(bars + BAR_ST);
-    };
-    // V scaled for the tile's own state (the last tile's is not needed); what lies behind the sequence's end becomes zero
-    float total = 0.f, total_next = 0.f;           // 2^(c_127) of the tile in hand and of the one ahead
-    auto put_scaled = [&](int j) {
-      const int s = j % NST, slot = j & (NSLOT - 1);
-      if (!warp_wait(bars + BAR_FULL + s, (j / NST) & 1, abort_flag) || !warp_wait(bars + BAR_DEC_FULL + slot, (j / NSLOT) & 1, abort_flag)) return false;
-      const float left = decays[slot].left[tok];
-      total_next = decays[slot].total;
+    float total = 0.f;                           // 2^(c of the tile) of the tile whose own state is awaited
+    int s = 0, round = 0;
+    // j: the tile whose V is scaled; the state after tile j - 2 goes on to the one after j - 1 (j = 0: the first is put in place)
+#pragma unroll 1
+    for (int j = 0; j < w.tiles && ok; ++j) {
+      const int slot = j & (NSLOT - 1), b = j & 1, xb = XB == 2 ? b : 0;
+      ok = warp_wait(bars + BAR_FULL + s, round & 1, abort_flag) && warp_wait(bars + BAR_DEC_FULL + slot, (j / NSLOT) & 1, abort_flag);
+      if (!ok) break;
+      const float left = decays[slot].left[tok], total_here = decays[slot].total;
       __syncwarp();
       if (lane == 0) mbar_arrive(bars + BAR_DEC_EMPTY + slot);
-      if (!warp_wait(bars + BAR_X_EMPTY + (XB == 2 ? (j & 1) : 0), ((XB == 2 ? j >> 1 : j) & 1) ^ 1, abort_flag)) return false;
-      const bool dead = w.t0 + j * CT + tok >= w.live;
-      if (dead) {
+      ok = warp_wait(bars + BAR_X_EMPTY + xb, ((XB == 2 ? j >> 1 : j) & 1) ^ 1, abort_flag);
+      if (!ok) break;
+      if (w.t0 + j * CT + tok >= w.live) {       // what lies behind the sequence's end becomes zero
         const uint4 z = make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
+#pragma unroll 1
         for (int c = 0; c < 8; ++c) {
           *reinterpret_cast<uint4*>(vtile(s) + tok * 128 + c * 16) = z;
 #pragma unroll
           for (int i = 0; i < Sh::HALVES; ++i) *reinterpret_cast<uint4*>(ktile(s) + i * HALF + tok * 128 + c * 16) = z;
         }
       }
-      if (j + 1 < w.tiles) {
+      if (j + 1 < w.tiles) {                     // (the last tile's own state is not needed)
         unsigned char *src = vtile(s), *dst = xtile(j);
-#pragma unroll
+#pragma unroll 4
         for (int c = 0; c < 8; ++c) {
           const uint32_t off = sw128_offset(tok, c);
           uint4 x[1];
@@ -442,32 +468,40 @@ tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
       }
       fence_async_smem();
-      mbar_arrive(bars + BAR_X_FULL + (XB == 2 ? (j & 1) : 0));
-      return true;
-    };
-    put_state();
-    if (w.tiles > 0) ok = put_scaled(0);
-    for (int j = 0; j < w.tiles - 1 && ok; ++j) {
-      total = total_next;
-      ok = put_scaled(j + 1);
-      if (!ok) break;
-      const int b = j & 1;
-      ok = warp_wait(bars + BAR_SL_FULL + b, (j >> 1) & 1, abort_flag);
-      if (!ok) break;
-      tc_fence_after();
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        uint32_t x[32];
-        tmem_ld32(tmem_addr(tb, q4 * 32, COL_SL + b * DV + hf * 32), x);
-        tmem_wait_ld(x);
-#pragma unroll
-        for (int c = 0; c < 32; ++c) S[hf * 32 + c] = fmaf(total, S[hf * 32 + c], __uint_as_float(x[c]));
+      mbar_arrive(bars + BAR_X_FULL + xb);
+      if (++s == NST) {
+        s = 0;
+        ++round;
       }
-      tc_fence_before();
-      mbar_arrive(bars + BAR_SL_EMPTY + b);
-      ok = warp_wait(bars + BAR_R_DONE, j & 1, abort_flag);
-      if (!ok) break;
-      put_state();
+      if (j > 0) {
+        const int bb = (j - 1) & 1;
+        ok = warp_wait(bars + BAR_SL_FULL + bb, ((j - 1) >> 1) & 1, abort_flag);
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          uint32_t x[32];
+          tmem_ld32(tmem_addr(tb, q4 * 32, COL_SL + bb * DV + hf * 32), x);
+          tmem_wait_ld(x);
+#pragma unroll
+          for (int c = 0; c < 16; ++c) S[hf * 16 + c] = fma2(make_float2(total, total), S[hf * 16 + c], f2(x[2 * c], x[2 * c + 1]));
+        }
+        tc_fence_before();
+        mbar_arrive(bars + BAR_SL_EMPTY + bb);
+        ok = warp_wait(bars + BAR_R_DONE, (j - 1) & 1, abort_flag);
+        if (!ok) break;
+      }
+      total = total_here;
+      if (mine) {                                // the bf16 copy that the Q S of tile j reads: [row][64 columns]
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          const float2* x = S + 4 * c;
+          *reinterpret_cast<uint4*>(base + Sh::OFF_S + sw128_offset(row, c)) =
+              make_uint4(pack_bf16(x[0].x, x[0].y), pack_bf16(x[1].x, x[1].y), pack_bf16(x[2].x, x[2].y), pack_bf16(x[3].x, x[3].y));
+        }
+      }
+      fence_async_smem();
+      mbar_arrive(bars + BAR_ST);
     }
   } else {
     // =========================== weights and epilogue (256 threads) ===========================
@@ -475,93 +509,108 @@ tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     const int ch = (warp - W_BLD0) >> 2;         // column half
     const int row = q4 * 32 + lane;              // token of the tile (= TMEM lane)
     const float skip = a.D != nullptr ? a.D[w.h] : 0.f;
-    float from_state[2] = {0.f, 0.f};            // 2^(c_t) of the tile's row, by parity of the tile
-    auto epilogue = [&](int j) {
-      if (!warp_wait(bars + BAR_O_FULL, j & 1, abort_flag)) return false;
-      tc_fence_after();
-      uint32_t y[32], r[32];
-      tmem_ld32(tmem_addr(tb, q4 * 32, COL_Y + ch * 32), y);
-      tmem_ld32(tmem_addr(tb, q4 * 32, COL_R + ch * 32), r);
-      tmem_wait_ld(y);
-      tmem_wait_ld(r);
-      tc_fence_before();
-      mbar_arrive(bars + BAR_O_EMPTY);
-      const float f = (j & 1) ? from_state[1] : from_state[0];
-      const bool dead = w.t0 + j * CT + row >= w.live;
-      unsigned char* rows = base + Sh::OFF_OUT + (warp - W_BLD0) * 2048;
-      if (lane == 0) bulk_wait_read();           // the store of the tile before has read them
-      __syncwarp();
+    unsigned char* rows = base + Sh::OFF_OUT + (warp - W_BLD0) * 2048;
+    float from_state = 0.f;                      // 2^(c_t) from the start of the tile
+    uint32_t xv[16];                             // this row's half of V, of the tile whose result is awaited
+    int s = 0, round = 0;
+#pragma unroll 1
+    for (int j = 0; j <= w.tiles && ok; ++j) {
+      float from_here = 0.f;
+      if (j < w.tiles) {
+        const int b = j & 1, slot = j & (NSLOT - 1);
+        ok = warp_wait(bars + BAR_DEC_FULL + slot, (j / NSLOT) & 1, abort_flag) && warp_wait(bars + BAR_S_FULL + b, (j >> 1) & 1, abort_flag);
+        if (!ok) break;
+        tc_fence_after();
+        const Decays& d = decays[slot];
+        const float rf = d.row[row];
+        from_here = rf * d.before[q4];
+        const uint32_t scol = tmem_addr(tb, q4 * 32, COL_P + b * 128 + ch * 64);
+#pragma unroll 1
+        for (int hf = 0; hf < 2; ++hf) {
+          const uint32_t blk = 2 * ch + hf;      // columns 32 blk .. of the tile, against rows 32 q4 ..
+          uint32_t pk[16];
+          if (blk > q4) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t o[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int e = 8 * c + 2 * i;
-          o[i] = pack_bf16(fmaf(f, __uint_as_float(r[e]), __uint_as_float(y[e])), fmaf(f, __uint_as_float(r[e + 1]), __uint_as_float(y[e + 1])));
-          if (dead) o[i] = 0u;
-        }
-        *reinterpret_cast<uint4*>(rows + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-      }
-      fence_async_smem();
-      __syncwarp();
-      if (lane == 0 && w.t0 + j * CT + (int)q4 * 32 < a.T) tma_store_4d(&tmO, rows, ch * 32, w.t0 + j * CT + q4 * 32, w.h, w.b);
-      return true;
-    };
-    for (int j = 0; j < w.tiles && ok; ++j) {
-      const int b = j & 1, slot = j & (NSLOT - 1);
-      ok = warp_wait(bars + BAR_DEC_FULL + slot, (j / NSLOT) & 1, abort_flag) && warp_wait(bars + BAR_S_FULL + b, (j >> 1) & 1, abort_flag);
-      if (!ok) break;
-      tc_fence_after();
-      const Decays& d = decays[slot];
-      const float rel = d.rel[row], rf = ex2(rel);
-      if (b) from_state[1] = rf * d.before[q4];
-      else from_state[0] = rf * d.before[q4];
-      const uint32_t scol = tmem_addr(tb, q4 * 32, COL_P + b * 128 + ch * 64);
-      const float* col = d.col + (q4 < 2 ? 0 : q4 == 2 ? 32 : 96);
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        const uint32_t blk = 2 * ch + hf;        // columns 32 blk .. of the tile, against rows 32 q4 ..
-        uint32_t pk[16];
-        if (blk > q4) {
-#pragma unroll
-          for (int c = 0; c < 16; ++c) pk[c] = 0u;
-        } else {
-          uint32_t y[32];
-          tmem_ld32(scol + hf * 32, y);
-          tmem_wait_ld(y);
-          if (blk == q4) {
-#pragma unroll
-            for (int c = 0; c < 32; c += 4) {
-              const float4 rs = *reinterpret_cast<const float4*>(d.rel + blk * 32 + c), st = *reinterpret_cast<const float4*>(d.step + blk * 32 + c);
-              const float rr[4] = {rs.x, rs.y, rs.z, rs.w}, ss[4] = {st.x, st.y, st.z, st.w};
-              float v[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                v[i] = __uint_as_float(y[c + i]) * (ss[i] * ex2(rel - rr[i]));
-                if (c + i == lane) v[i] += skip;
-                if (c + i > lane) v[i] = 0.f;
-              }
-              pk[c / 2] = pack_bf16(v[0], v[1]);
-              pk[c / 2 + 1] = pack_bf16(v[2], v[3]);
-            }
+            for (int c = 0; c < 16; ++c) pk[c] = 0u;
           } else {
+            uint32_t y[32];
+            tmem_ld32(scol + hf * 32, y);
+            tmem_wait_ld(y);
+            const bool diag = blk == q4;
+            if (diag && ((d.steep >> blk) & 1)) {
+              const float rel = d.rel[row];
 #pragma unroll
-            for (int c = 0; c < 32; c += 4) {
-              const float4 cf = *reinterpret_cast<const float4*>(col + blk * 32 + c);
-              pk[c / 2] = pack_bf16(__uint_as_float(y[c]) * (cf.x * rf), __uint_as_float(y[c + 1]) * (cf.y * rf));
-              pk[c / 2 + 1] = pack_bf16(__uint_as_float(y[c + 2]) * (cf.z * rf), __uint_as_float(y[c + 3]) * (cf.w * rf));
+              for (int c = 0; c < 32; c += 2)
+                pk[c / 2] = pack_bf16(__uint_as_float(y[c]) * (d.step[blk * 32 + c] * ex2(rel - d.rel[blk * 32 + c])),
+                                      __uint_as_float(y[c + 1]) * (d.step[blk * 32 + c + 1] * ex2(rel - d.rel[blk * 32 + c + 1])));
+            } else {
+              const float4* col = reinterpret_cast<const float4*>((diag ? d.inv : d.tail) + blk * 32);
+              const float f = diag ? rf : rf * d.between[q4][blk];
+              const float2 ff = make_float2(f, f);
+#pragma unroll
+              for (int c = 0; c < 32; c += 4) {
+                const float4 cf = col[c / 4];
+                const float2 u = mul2(mul2(make_float2(cf.x, cf.y), ff), f2(y[c], y[c + 1])), v = mul2(mul2(make_float2(cf.z, cf.w), ff), f2(y[c + 2], y[c + 3]));
+                pk[c / 2] = pack_bf16(u.x, u.y);
+                pk[c / 2 + 1] = pack_bf16(v.x, v.y);
+              }
+            }
+            if (diag) {                          // column c counts for rows c and behind
+#pragma unroll
+              for (int c = 0; c < 16; ++c) pk[c] = 2 * c + 1 <= lane ? pk[c] : 2 * c == lane ? pk[c] & 0xffffu : 0u;
             }
           }
+          tmem_st16(scol + hf * 16, pk);
         }
-        tmem_st16(scol + hf * 16, pk);
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(bars + BAR_P_FULL + b);
+        if (lane == 0) mbar_arrive(bars + BAR_DEC_EMPTY + slot);
       }
-      tmem_wait_st();
-      tc_fence_before();
-      mbar_arrive(bars + BAR_P_FULL + b);
-      if (lane == 0) mbar_arrive(bars + BAR_DEC_EMPTY + slot);
-      if (j > 0) ok = epilogue(j - 1);
+      if (j > 0) {
+        ok = warp_wait(bars + BAR_O_FULL, (j - 1) & 1, abort_flag);
+        if (!ok) break;
+        tc_fence_after();
+        uint32_t y[32], r[32];
+        tmem_ld32(tmem_addr(tb, q4 * 32, COL_Y + ch * 32), y);
+        tmem_ld32(tmem_addr(tb, q4 * 32, COL_R + ch * 32), r);
+        tmem_wait_ld(y);
+        tmem_wait_ld(r);
+        tc_fence_before();
+        mbar_arrive(bars + BAR_O_EMPTY);
+        const bool dead = w.t0 + (j - 1) * CT + row >= w.live;
+        if (lane == 0) bulk_wait_read();         // the store of the tile before has read the staging rows
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t o[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int e = 8 * c + 2 * i;
+            const float2 z = fma2(unpack(xv[e / 2]), make_float2(skip, skip), fma2(make_float2(from_state, from_state), f2(r[e], r[e + 1]), f2(y[e], y[e + 1])));
+            o[i] = dead ? 0u : pack_bf16(z.x, z.y);
+          }
+          *reinterpret_cast<uint4*>(rows + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+        fence_async_smem();
+        __syncwarp();
+        const int first = w.t0 + (j - 1) * CT + (int)q4 * 32;
+        if (lane == 0 && first < a.T) tma_store_4d(&tmO, rows, ch * 32, first, w.h, w.b);
+      }
+      if (j < w.tiles) {
+        from_state = from_here;
+        ok = warp_wait(bars + BAR_FULL + s, round & 1, abort_flag);
+        if (!ok) break;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) *reinterpret_cast<uint4*>(xv + 4 * c) = *reinterpret_cast<const uint4*>(vtile(s) + sw128_offset(row, ch * 4 + c));
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bars + BAR_EMPTY + s);
+        if (++s == NST) {
+          s = 0;
+          ++round;
+        }
+      }
     }
-    if (ok && w.tiles > 0) ok = epilogue(w.tiles - 1);
   }
 
   // ---------------- teardown ----------------
@@ -671,9 +720,10 @@ tc_ssm_state_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   } else if (warp >= W_STATE0 && warp < W_BLD0) {
     // =========================== state ===========================
     const int q4 = warp & 3, row = state_row<N>(q4, lane);
-    float S[DV];
+    float2 S[DV / 2];
 #pragma unroll
-    for (int c = 0; c < DV; ++c) S[c] = 0.f;
+    for (int c = 0; c < DV / 2; ++c) S[c] = make_float2(0.f, 0.f);
+#pragma unroll 1
     for (int j = 0; j < w.tiles && ok; ++j) {
       const int b = j & 1, slot = j & (NSLOT - 1);
       ok = warp_wait(bars + BAR_DEC_FULL + slot, (j / NSLOT) & 1, abort_flag);
@@ -689,7 +739,7 @@ tc_ssm_state_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
         tmem_ld32(tmem_addr(tb, q4 * 32, COL_SL + b * DV + hf * 32), x);
         tmem_wait_ld(x);
 #pragma unroll
-        for (int c = 0; c < 32; ++c) S[hf * 32 + c] = fmaf(total, S[hf * 32 + c], __uint_as_float(x[c]));
+        for (int c = 0; c < 16; ++c) S[hf * 16 + c] = fma2(make_float2(total, total), S[hf * 16 + c], f2(x[2 * c], x[2 * c + 1]));
       }
       tc_fence_before();
       mbar_arrive(bars + BAR_SL_EMPTY + b);
@@ -697,7 +747,7 @@ tc_ssm_state_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
     if (state_lane<N>(lane)) {
       float4* dst = reinterpret_cast<float4*>(a.local + ((size_t)w.bh * a.slots + w.seg + 1) * (N * DV) + (size_t)row * DV);
 #pragma unroll
-      for (int c = 0; c < DV / 4; ++c) dst[c] = make_float4(S[4 * c], S[4 * c + 1], S[4 * c + 2], S[4 * c + 3]);
+      for (int c = 0; c < DV / 4; ++c) dst[c] = make_float4(S[2 * c].x, S[2 * c].y, S[2 * c + 1].x, S[2 * c + 1].y);
     }
   } else if (warp >= W_BLD0) {
     // =========================== scaled V in three terms ===========================
