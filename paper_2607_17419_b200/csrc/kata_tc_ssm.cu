@@ -175,12 +175,12 @@ __device__ __forceinline__ double decay_warp(const Args& a, const Where& w, Deca
   const float rate = (float)((double)a.A[w.h] * 1.4426950408889634074);
   const float bias = a.dt_bias != nullptr ? a.dt_bias[w.h] : 0.f;
   double all = 0.0;
-  float next[4];
+  __nv_bfloat16 next[4];                         // (as they come: nothing waits for them before the next tile)
   auto fetch = [&](int j) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int t = w.t0 + j * CT + lane * 4 + i;
-      next[i] = t < w.live ? __bfloat162float(dt[(long long)t * a.dt2]) + bias : 0.f;
+      next[i] = dt[(long long)min(t, w.live - 1) * a.dt2];
     }
   };
   if (w.tiles > 0) fetch(0);
@@ -189,7 +189,8 @@ __device__ __forceinline__ double decay_warp(const Args& a, const Where& w, Deca
     float s[4], c[4], sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      s[i] = !a.softplus || next[i] > 20.f ? next[i] : log1pf(expf(next[i]));
+      const float x = __bfloat162float(next[i]) + bias;
+      s[i] = a.softplus ? softplus(x) : x;
       if (w.t0 + j * CT + lane * 4 + i >= w.live) s[i] = 0.f;
       sum = fmaf(s[i], rate, sum);
       c[i] = sum;
