@@ -6,17 +6,17 @@
 //
 // tc_ssm_out_kernel: a CTA has one head and a segment of its tokens and walks the tiles.  Scores come from the tensor cores,
 // builder warps weigh them in registers and put them back into TMEM as the bf16 A operand of the product with V.  Nothing but
-// S ties the tiles together: its fp32 entries stay in the registers of four warps, which add the tile's own state (a product of
+// S ties the tiles together: its fp32 entries stay in TMEM, where four warps add the tile's own state (a product of
 // its own, from V scaled and rounded to bf16) and leave a bf16 copy in shared memory for the next tile's Q S.
 // The weights of a 32 x 32 block are a row factor times a column factor, taken at the start of the rows' block: below the diagonal
-// both are at most s_i, on the diagonal the column factor is 2^(-c_i) s_i, and blocks that decay by more than 2^-100 in their 32
-// tokens take an exponential per entry instead.  So a tile takes a few exponentials per token and two products per score.
+// both are at most s_i; on the diagonal they are taken at half of the block's decay, and only blocks that decay by more than 2^-240 in
+// their 32 tokens take an exponential per entry instead.  So a tile takes a few exponentials per token and two products per score.
 // tc_ssm_state_kernel: the segments' own states (several segments, or a final state wanted), exact to fp32: the scaled V goes in
 // as three bf16 terms (24 bits), the small ones first, and every tile's product is added in registers.
 //
-// Warps (512 threads).  Out: 0 decays; 1 issues Q K^T and Q S, 2 the tile's state and the product with V; 3 TMA loads;
-// 4-7 scaled V, state; 8-15 weights and epilogue (two warps per TMEM lane quadrant).  State: 8-15 scaled V.  The roles' loops are
-// written once each and kept short: sixteen warps in unlike code of some thousand instructions each waited for instructions most of
+// Warps.  Out (768 threads): 0 decays; 1 issues Q K^T and Q S, 2 the tile's state and the product with V; 3 TMA loads;
+// 4-7 state; 8-15 weights and 16-23 scaled V and epilogue, two warps per TMEM lane quadrant.  State (512): 8-15 scaled V.  A warp reaches the next wait of its job long before the
+// others are done with theirs, so a tile takes the longest job and not their sum.  The jobs' loops are written once each and kept short: sixteen warps in unlike code of some thousand instructions each waited for instructions most of
 // the time (8 x 16 heads x 4096 tokens 135 us).  All waits are bounded; a warp that has TMEM to read goes on only where all its
 // lanes saw the barrier.
 #include <cuda.h>
@@ -33,8 +33,8 @@ using namespace umma;
 
 constexpr int CT = 128;                          // tokens per tile
 constexpr int DV = 64;
-constexpr int NTHREADS = 512;
-constexpr int W_STATE0 = 4, W_BLD0 = 8;
+constexpr int kOutThreads = 768, kStateThreads = 512;
+constexpr int W_STATE0 = 4, W_WEIGHT0 = 8, W_OUT0 = 16;
 constexpr uint32_t HALF = 16384;                 // 128 rows of 64 bf16 entries, 128B swizzle
 constexpr int NSLOT = 4;                         // tiles whose decays are held
 
@@ -42,13 +42,14 @@ constexpr int NSLOT = 4;                         // tiles whose decays are held
 struct Decays {
   float row[CT];                                 // 2^(c_t)
   float tail[CT];                                // 2^(c at the end of the block - c_t) s_t
-  float inv[CT];                                 // 2^(-c_t) s_t
+  float inv[CT];                                 // 2^(m - c_t) s_t, m half of c at the end of the block
   float left[CT];                                // 2^(c at the end of the tile - c_t) s_t
   float rel[CT], step[CT];                       // c_t, s_t
   float before[4];                               // 2^(c from the start of the tile to block b)
   float between[4][4];                           // [r][b]: 2^(c from the end of block b to the start of block r), b < r
   float total;                                   // 2^(c of the whole tile)
-  int steep;                                     // bit b: block b decays (or grows) by more than 2^100
+  int steep;                                     // bit b: block b decays (or grows) by more than 2^240
+  float half[4];                                 // m
   float pad[2];
 };
 
@@ -72,7 +73,7 @@ static_assert(Shape<64, false>::SMEM > 116 * 1024 && Shape<64, true>::SMEM > 116
 
 constexpr uint32_t COL_P = 0;                    // 2 x 128: scores; the bf16 weights overwrite columns [0,32) and [64,96) of a buffer
 constexpr uint32_t COL_Y = 256, COL_R = 320;     // product with V, Q S
-constexpr uint32_t COL_SL = 384;                 // 2 x 64: own state of a tile
+constexpr uint32_t COL_SL = 384, COL_S = 448;    // own state of a tile, state (state kernel: 2 x 64, own states)
 constexpr uint32_t TMEM_COLS = 512;
 
 // Every barrier's phases are seen in order by all that wait for it before the next can complete (see the notes at the waits).
@@ -146,7 +147,7 @@ __device__ __forceinline__ float2 unpack(uint32_t x) { return f2(x << 16, x & 0x
 
 // The wait of a whole warp: all lanes, or none.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-  return __all_sync(0xffffffffu, wait_or_abort_counted(bar, parity, abort_flag));
+  return __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort_flag));
 }
 
 struct Where {
@@ -219,12 +220,14 @@ __device__ __forceinline__ double decay_warp(const Args& a, const Where& w, Deca
     }
     reinterpret_cast<float4*>(d.left)[lane] = make_float4(tail[0] * behind, tail[1] * behind, tail[2] * behind, tail[3] * behind);
     if (ALL) {
+      const float m = 0.5f * mine;
       reinterpret_cast<float4*>(d.tail)[lane] = make_float4(tail[0], tail[1], tail[2], tail[3]);
       reinterpret_cast<float4*>(d.row)[lane] = make_float4(ex2(c[0]), ex2(c[1]), ex2(c[2]), ex2(c[3]));
-      reinterpret_cast<float4*>(d.inv)[lane] = make_float4(s[0] * ex2(-c[0]), s[1] * ex2(-c[1]), s[2] * ex2(-c[2]), s[3] * ex2(-c[3]));
+      reinterpret_cast<float4*>(d.inv)[lane] = make_float4(s[0] * ex2(m - c[0]), s[1] * ex2(m - c[1]), s[2] * ex2(m - c[2]), s[3] * ex2(m - c[3]));
       reinterpret_cast<float4*>(d.rel)[lane] = make_float4(c[0], c[1], c[2], c[3]);
       reinterpret_cast<float4*>(d.step)[lane] = make_float4(s[0], s[1], s[2], s[3]);
-      const unsigned steep = __ballot_sync(0xffffffffu, !(fabsf(c[0]) < 100.f && fabsf(c[1]) < 100.f && fabsf(c[2]) < 100.f && fabsf(c[3]) < 100.f));
+      const unsigned steep = __ballot_sync(0xffffffffu, !(fabsf(c[0] - m) < 120.f && fabsf(c[1] - m) < 120.f && fabsf(c[2] - m) < 120.f && fabsf(c[3] - m) < 120.f));
+      if ((lane & 7) == 0) d.half[blk] = m;
       // lanes 0-3: before; 4: the whole tile; 5: [2][0], 6: [3][0], 7: [3][1]; neighbours are 1
       const float e = ex2(lane == 1 ? b0 : lane == 2 ? b0 + b1 : lane == 3 ? b0 + b1 + b2 : lane == 4 ? (b0 + b1) + (b2 + b3) : lane == 5 ? b1
                           : lane == 6 ? b1 + b2 : lane == 7 ? b2 : 0.f);
@@ -270,7 +273,7 @@ template <int N> __device__ __forceinline__ int state_row(int q4, int lane) { re
 template <int N> __device__ __forceinline__ bool state_lane(int lane) { return N == 128 || lane < 16; }
 
 template <int N>
-__global__ void __launch_bounds__(NTHREADS, 1)
+__global__ void __launch_bounds__(kOutThreads, 1)
 tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                   const __grid_constant__ CUtensorMap tmO, const __grid_constant__ Args a) {
   typedef Shape<N, false> Sh;
@@ -295,9 +298,9 @@ tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       uint32_t n = 1;
       if (i >= BAR_EMPTY && i < BAR_EMPTY + 3) n = 2 + 8;
       if (i >= BAR_DEC_FULL && i < BAR_DEC_FULL + NSLOT) n = 32;
-      if (i >= BAR_DEC_EMPTY && i < BAR_DEC_EMPTY + NSLOT) n = 12;
-      if (i == BAR_P_FULL || i == BAR_P_FULL + 1 || i == BAR_O_EMPTY) n = 256;
-      if (i == BAR_X_FULL || i == BAR_X_FULL + 1 || i == BAR_SL_EMPTY || i == BAR_SL_EMPTY + 1 || i == BAR_ST) n = 128;
+      if (i >= BAR_DEC_EMPTY && i < BAR_DEC_EMPTY + NSLOT) n = 4 + 8 + 8;
+      if (i == BAR_P_FULL || i == BAR_P_FULL + 1 || i == BAR_O_EMPTY || i == BAR_X_FULL || i == BAR_X_FULL + 1) n = 256;
+      if (i == BAR_SL_EMPTY || i == BAR_ST) n = 128;
       if (i == BAR_O_FULL || i == BAR_DRAIN) n = 2;
       mbar_init(bars + i, n);
     }
@@ -376,14 +379,14 @@ tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       ok = warp_wait(bars + BAR_FULL + s, round & 1, abort_flag) &&
            warp_wait(bars + BAR_X_FULL + (XB == 2 ? b : 0), (XB == 2 ? j >> 1 : j) & 1, abort_flag);
       if (ok && j + 1 < w.tiles) {
-        ok = warp_wait(bars + BAR_SL_EMPTY + b, ((j >> 1) & 1) ^ 1, abort_flag);
+        ok = warp_wait(bars + BAR_SL_EMPTY, (j & 1) ^ 1, abort_flag);
         if (!ok) break;
         if (elect_one()) {
           const uint32_t ka = smem_u32(ktile(s)), xa = smem_u32(xtile(j));
           tc_fence_after();
 #pragma unroll
-          for (int ks = 0; ks < CT / 16; ++ks) mma_f16_ss(tb + COL_SL + b * DV, at(dn, ka + ks * 2048), at(dn, xa + ks * 2048), id_s, ks > 0);
-          mma_commit(bars + BAR_SL_FULL + b);
+          for (int ks = 0; ks < CT / 16; ++ks) mma_f16_ss(tb + COL_SL, at(dn, ka + ks * 2048), at(dn, xa + ks * 2048), id_s, ks > 0);
+          mma_commit(bars + BAR_SL_FULL);
           mma_commit(bars + BAR_X_EMPTY + (XB == 2 ? b : 0));
         }
         __syncwarp();
@@ -411,7 +414,7 @@ tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     if (lane == 0) {
       for (int j = 0; j < w.tiles && ok; ++j) {
         const int s = j % NST, tok = w.t0 + j * CT;
-        ok = wait_or_abort_counted(bars + BAR_EMPTY + s, ((j / NST) & 1) ^ 1, abort_flag);
+        ok = wait_or_abort(bars + BAR_EMPTY + s, ((j / NST) & 1) ^ 1, abort_flag);
         if (!ok) break;
         mbar_arrive_expect_tx(bars + BAR_FULL + s, Sh::STAGE);
 #pragma unroll
@@ -422,194 +425,208 @@ tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         tma_load_4d(vtile(s), &tmV, bars + BAR_FULL + s, 0, tok, w.h * a.vh, w.b * a.vb);
       }
     }
-  } else if (warp < W_BLD0) {
-    // =========================== scaled V, state ===========================
-    const int q4 = warp & 3, row = state_row<N>(q4, lane), tok = q4 * 32 + lane;
+  } else if (warp < W_WEIGHT0) {
+    // =========================== state ===========================
+    // fp32 in TMEM (in registers it would take 64 of a thread's 80)
+    const int q4 = warp & 3, row = state_row<N>(q4, lane);
     const bool mine = state_lane<N>(lane);
-    float2 S[DV / 2];
-    {
-      const float* src = a.init != nullptr ? a.init + ((size_t)w.bh * a.slots + w.seg) * (N * DV) + (size_t)row * DV : nullptr;
-#pragma unroll
-      for (int c = 0; c < DV; c += 4) {
-        const float4 x = mine && src != nullptr ? *reinterpret_cast<const float4*>(src + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-        S[c / 2] = make_float2(x.x, x.y);
-        S[c / 2 + 1] = make_float2(x.z, x.w);
-      }
-    }
-    float total = 0.f;                           // 2^(c of the tile) of the tile whose own state is awaited
-    int s = 0, round = 0;
-    // j: the tile whose V is scaled; the state after tile j - 2 goes on to the one after j - 1 (j = 0: the first is put in place)
+    const uint32_t scol = tmem_addr(tb, q4 * 32, COL_S), lcol = tmem_addr(tb, q4 * 32, COL_SL);
+    const float* src = a.init != nullptr ? a.init + ((size_t)w.bh * a.slots + w.seg) * (N * DV) + (size_t)row * DV : nullptr;
+    // j: the tile that the state goes before (0: as handed in; then the own state of tile j - 1 is added)
 #pragma unroll 1
     for (int j = 0; j < w.tiles && ok; ++j) {
-      const int slot = j & (NSLOT - 1), b = j & 1, xb = XB == 2 ? b : 0;
-      ok = warp_wait(bars + BAR_FULL + s, round & 1, abort_flag) && warp_wait(bars + BAR_DEC_FULL + slot, (j / NSLOT) & 1, abort_flag);
-      if (!ok) break;
-      const float left = decays[slot].left[tok], total_here = decays[slot].total;
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bars + BAR_DEC_EMPTY + slot);
-      ok = warp_wait(bars + BAR_X_EMPTY + xb, ((XB == 2 ? j >> 1 : j) & 1) ^ 1, abort_flag);
-      if (!ok) break;
-      if (w.t0 + j * CT + tok >= w.live) {       // what lies behind the sequence's end becomes zero
-        const uint4 z = make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll 1
-        for (int c = 0; c < 8; ++c) {
-          *reinterpret_cast<uint4*>(vtile(s) + tok * 128 + c * 16) = z;
-#pragma unroll
-          for (int i = 0; i < Sh::HALVES; ++i) *reinterpret_cast<uint4*>(ktile(s) + i * HALF + tok * 128 + c * 16) = z;
-        }
-      }
-      if (j + 1 < w.tiles) {                     // (the last tile's own state is not needed)
-        unsigned char *src = vtile(s), *dst = xtile(j);
-#pragma unroll 4
-        for (int c = 0; c < 8; ++c) {
-          const uint32_t off = sw128_offset(tok, c);
-          uint4 x[1];
-          scaled_terms<1>(*reinterpret_cast<const uint4*>(src + off), left, x);
-          *reinterpret_cast<uint4*>(dst + off) = x[0];
-        }
-      }
-      fence_async_smem();
-      mbar_arrive(bars + BAR_X_FULL + xb);
-      if (++s == NST) {
-        s = 0;
-        ++round;
-      }
+      float total = 0.f;
       if (j > 0) {
-        const int bb = (j - 1) & 1;
-        ok = warp_wait(bars + BAR_SL_FULL + bb, ((j - 1) >> 1) & 1, abort_flag);
+        const int slot = (j - 1) & (NSLOT - 1);
+        ok = warp_wait(bars + BAR_DEC_FULL + slot, ((j - 1) / NSLOT) & 1, abort_flag);
+        if (!ok) break;
+        total = decays[slot].total;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bars + BAR_DEC_EMPTY + slot);
+        ok = warp_wait(bars + BAR_SL_FULL, (j - 1) & 1, abort_flag) && warp_wait(bars + BAR_R_DONE, (j - 1) & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          uint32_t x[32];
-          tmem_ld32(tmem_addr(tb, q4 * 32, COL_SL + bb * DV + hf * 32), x);
+      }
+      const float2 keep = make_float2(total, total);
+#pragma unroll 1
+      for (int p = 0; p < 4; ++p) {
+        uint32_t S[16];
+        if (j > 0) {
+          uint32_t x[16];
+          tmem_ld16(scol + p * 16, S);
+          tmem_ld16(lcol + p * 16, x);
+          tmem_wait_ld(S);
           tmem_wait_ld(x);
 #pragma unroll
-          for (int c = 0; c < 16; ++c) S[hf * 16 + c] = fma2(make_float2(total, total), S[hf * 16 + c], f2(x[2 * c], x[2 * c + 1]));
-        }
-        tc_fence_before();
-        mbar_arrive(bars + BAR_SL_EMPTY + bb);
-        ok = warp_wait(bars + BAR_R_DONE, (j - 1) & 1, abort_flag);
-        if (!ok) break;
-      }
-      total = total_here;
-      if (mine) {                                // the bf16 copy that the Q S of tile j reads: [row][64 columns]
+          for (int c = 0; c < 16; c += 2) {
+            const float2 n = fma2(keep, f2(S[c], S[c + 1]), f2(x[c], x[c + 1]));
+            S[c] = __float_as_uint(n.x);
+            S[c + 1] = __float_as_uint(n.y);
+          }
+        } else {
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          const float2* x = S + 4 * c;
-          *reinterpret_cast<uint4*>(base + Sh::OFF_S + sw128_offset(row, c)) =
-              make_uint4(pack_bf16(x[0].x, x[0].y), pack_bf16(x[1].x, x[1].y), pack_bf16(x[2].x, x[2].y), pack_bf16(x[3].x, x[3].y));
+          for (int c = 0; c < 16; c += 4) {
+            const float4 x = mine && src != nullptr ? *reinterpret_cast<const float4*>(src + p * 16 + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+            S[c] = __float_as_uint(x.x);
+            S[c + 1] = __float_as_uint(x.y);
+            S[c + 2] = __float_as_uint(x.z);
+            S[c + 3] = __float_as_uint(x.w);
+          }
+        }
+        tmem_st16(scol + p * 16, S);
+        if (mine) {                              // the bf16 copy that the Q S of tile j reads: [row][64 columns]
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            uint32_t o[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = pack_bf16(__uint_as_float(S[8 * c + 2 * i]), __uint_as_float(S[8 * c + 2 * i + 1]));
+            *reinterpret_cast<uint4*>(base + Sh::OFF_S + sw128_offset(row, 2 * p + c)) = make_uint4(o[0], o[1], o[2], o[3]);
+          }
         }
       }
+      tmem_wait_st();
+      tc_fence_before();
+      if (j > 0) mbar_arrive(bars + BAR_SL_EMPTY);
       fence_async_smem();
       mbar_arrive(bars + BAR_ST);
     }
-  } else {
-    // =========================== weights and epilogue (256 threads) ===========================
+  } else if (warp < W_OUT0) {
+    // =========================== weights (256 threads) ===========================
     const uint32_t q4 = warp & 3;
-    const int ch = (warp - W_BLD0) >> 2;         // column half
+    const int ch = (warp - W_WEIGHT0) >> 2;      // column half
+    const int row = q4 * 32 + lane;              // token of the tile (= TMEM lane)
+#pragma unroll 1
+    for (int j = 0; j < w.tiles && ok; ++j) {
+      const int b = j & 1, slot = j & (NSLOT - 1);
+      ok = warp_wait(bars + BAR_DEC_FULL + slot, (j / NSLOT) & 1, abort_flag) && warp_wait(bars + BAR_S_FULL + b, (j >> 1) & 1, abort_flag);
+      if (!ok) break;
+      tc_fence_after();
+      const Decays& d = decays[slot];
+      const float rf = d.row[row], rel = d.rel[row];
+      const uint32_t scol = tmem_addr(tb, q4 * 32, COL_P + b * 128 + ch * 64);
+      // Blocks of 32 columns; the bf16 weights go over the scores of this thread's half, which have been read by then.
+#pragma unroll 1
+      for (int hf = 0; hf < 2; ++hf) {
+        const uint32_t blk = 2 * ch + hf;
+        uint32_t pk[16];
+        if (blk > q4) {
+#pragma unroll
+          for (int c = 0; c < 16; ++c) pk[c] = 0u;
+        } else {
+          uint32_t y[32];
+          tmem_ld32(scol + hf * 32, y);
+          const bool diag = blk == q4;
+          const float4* col = reinterpret_cast<const float4*>((diag ? d.inv : d.tail) + blk * 32);
+          const float f = diag ? ex2(rel - d.half[blk]) : rf * d.between[q4][blk];
+          const float2 ff = make_float2(f, f);
+          tmem_wait_ld(y);
+          if (diag && ((d.steep >> blk) & 1)) {
+#pragma unroll
+            for (int c = 0; c < 32; c += 2)
+              pk[c / 2] = pack_bf16(__uint_as_float(y[c]) * (d.step[blk * 32 + c] * ex2(rel - d.rel[blk * 32 + c])),
+                                    __uint_as_float(y[c + 1]) * (d.step[blk * 32 + c + 1] * ex2(rel - d.rel[blk * 32 + c + 1])));
+          } else {
+#pragma unroll
+            for (int c = 0; c < 32; c += 4) {
+              const float4 cf = col[c / 4];
+              const float2 u = mul2(mul2(make_float2(cf.x, cf.y), ff), f2(y[c], y[c + 1])), v = mul2(mul2(make_float2(cf.z, cf.w), ff), f2(y[c + 2], y[c + 3]));
+              pk[c / 2] = pack_bf16(u.x, u.y);
+              pk[c / 2 + 1] = pack_bf16(v.x, v.y);
+            }
+          }
+          if (diag) {                            // column c counts for rows c and behind
+#pragma unroll
+            for (int c = 0; c < 16; ++c) pk[c] = 2 * c + 1 <= lane ? pk[c] : 2 * c == lane ? pk[c] & 0xffffu : 0u;
+          }
+        }
+        tmem_st16(scol + hf * 16, pk);
+      }
+      tmem_wait_st();
+      tc_fence_before();
+      mbar_arrive(bars + BAR_P_FULL + b);
+      if (lane == 0) mbar_arrive(bars + BAR_DEC_EMPTY + slot);
+    }
+  } else {
+    // =========================== scaled V, epilogue (256 threads) ===========================
+    const uint32_t q4 = warp & 3;
+    const int ch = (warp - W_OUT0) >> 2;         // column half
     const int row = q4 * 32 + lane;              // token of the tile (= TMEM lane)
     const float skip = a.D != nullptr ? a.D[w.h] : 0.f;
-    unsigned char* rows = base + Sh::OFF_OUT + (warp - W_BLD0) * 2048;
+    unsigned char* rows = base + Sh::OFF_OUT + (warp - W_OUT0) * 2048;
     float from_state = 0.f;                      // 2^(c_t) from the start of the tile
-    uint32_t xv[16];                             // this row's half of V, of the tile whose result is awaited
-    int s = 0, round = 0;
+    int s = 0, s_before = 0, round = 0;
 #pragma unroll 1
     for (int j = 0; j <= w.tiles && ok; ++j) {
       float from_here = 0.f;
       if (j < w.tiles) {
-        const int b = j & 1, slot = j & (NSLOT - 1);
-        ok = warp_wait(bars + BAR_DEC_FULL + slot, (j / NSLOT) & 1, abort_flag) && warp_wait(bars + BAR_S_FULL + b, (j >> 1) & 1, abort_flag);
+        const int b = j & 1, slot = j & (NSLOT - 1), xb = XB == 2 ? b : 0;
+        ok = warp_wait(bars + BAR_FULL + s, round & 1, abort_flag) && warp_wait(bars + BAR_DEC_FULL + slot, (j / NSLOT) & 1, abort_flag) &&
+             warp_wait(bars + BAR_X_EMPTY + xb, ((XB == 2 ? j >> 1 : j) & 1) ^ 1, abort_flag);
         if (!ok) break;
-        tc_fence_after();
-        const Decays& d = decays[slot];
-        const float rf = d.row[row];
-        from_here = rf * d.before[q4];
-        const uint32_t scol = tmem_addr(tb, q4 * 32, COL_P + b * 128 + ch * 64);
-#pragma unroll 1
-        for (int hf = 0; hf < 2; ++hf) {
-          const uint32_t blk = 2 * ch + hf;      // columns 32 blk .. of the tile, against rows 32 q4 ..
-          uint32_t pk[16];
-          if (blk > q4) {
-#pragma unroll
-            for (int c = 0; c < 16; ++c) pk[c] = 0u;
-          } else {
-            uint32_t y[32];
-            tmem_ld32(scol + hf * 32, y);
-            tmem_wait_ld(y);
-            const bool diag = blk == q4;
-            if (diag && ((d.steep >> blk) & 1)) {
-              const float rel = d.rel[row];
-#pragma unroll
-              for (int c = 0; c < 32; c += 2)
-                pk[c / 2] = pack_bf16(__uint_as_float(y[c]) * (d.step[blk * 32 + c] * ex2(rel - d.rel[blk * 32 + c])),
-                                      __uint_as_float(y[c + 1]) * (d.step[blk * 32 + c + 1] * ex2(rel - d.rel[blk * 32 + c + 1])));
-            } else {
-              const float4* col = reinterpret_cast<const float4*>((diag ? d.inv : d.tail) + blk * 32);
-              const float f = diag ? rf : rf * d.between[q4][blk];
-              const float2 ff = make_float2(f, f);
-#pragma unroll
-              for (int c = 0; c < 32; c += 4) {
-                const float4 cf = col[c / 4];
-                const float2 u = mul2(mul2(make_float2(cf.x, cf.y), ff), f2(y[c], y[c + 1])), v = mul2(mul2(make_float2(cf.z, cf.w), ff), f2(y[c + 2], y[c + 3]));
-                pk[c / 2] = pack_bf16(u.x, u.y);
-                pk[c / 2 + 1] = pack_bf16(v.x, v.y);
-              }
-            }
-            if (diag) {                          // column c counts for rows c and behind
-#pragma unroll
-              for (int c = 0; c < 16; ++c) pk[c] = 2 * c + 1 <= lane ? pk[c] : 2 * c == lane ? pk[c] & 0xffffu : 0u;
-            }
-          }
-          tmem_st16(scol + hf * 16, pk);
-        }
-        tmem_wait_st();
-        tc_fence_before();
-        mbar_arrive(bars + BAR_P_FULL + b);
+        const float left = decays[slot].left[row];
+        from_here = decays[slot].row[row] * decays[slot].before[q4];
+        __syncwarp();
         if (lane == 0) mbar_arrive(bars + BAR_DEC_EMPTY + slot);
+        const bool dead = w.t0 + j * CT + row >= w.live;
+#pragma unroll 2
+        for (int c = 4 * ch; c < 4 * ch + 4; ++c) {
+          const uint32_t off = sw128_offset(row, c);
+          uint4 x[1], v = *reinterpret_cast<const uint4*>(vtile(s) + off);
+          if (dead) {                            // what lies behind the sequence's end becomes zero
+            v = make_uint4(0u, 0u, 0u, 0u);
+            *reinterpret_cast<uint4*>(vtile(s) + off) = v;
+#pragma unroll
+            for (int i = 0; i < Sh::HALVES; ++i) *reinterpret_cast<uint4*>(ktile(s) + i * HALF + off) = v;
+          }
+          scaled_terms<1>(v, left, x);
+          *reinterpret_cast<uint4*>(xtile(j) + off) = x[0];
+        }
+        fence_async_smem();
+        mbar_arrive(bars + BAR_X_FULL + xb);
       }
       if (j > 0) {
         ok = warp_wait(bars + BAR_O_FULL, (j - 1) & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
-        uint32_t y[32], r[32];
-        tmem_ld32(tmem_addr(tb, q4 * 32, COL_Y + ch * 32), y);
-        tmem_ld32(tmem_addr(tb, q4 * 32, COL_R + ch * 32), r);
-        tmem_wait_ld(y);
-        tmem_wait_ld(r);
-        tc_fence_before();
-        mbar_arrive(bars + BAR_O_EMPTY);
-        const bool dead = w.t0 + (j - 1) * CT + row >= w.live;
         if (lane == 0) bulk_wait_read();         // the store of the tile before has read the staging rows
         __syncwarp();
+        const bool dead = w.t0 + (j - 1) * CT + row >= w.live;
+        const float2 f = make_float2(from_state, from_state), sk = make_float2(skip, skip);
+#pragma unroll 1
+        for (int p = 0; p < 2; ++p) {
+          uint32_t y[16], r[16];
+          tmem_ld16(tmem_addr(tb, q4 * 32, COL_Y + ch * 32 + p * 16), y);
+          tmem_ld16(tmem_addr(tb, q4 * 32, COL_R + ch * 32 + p * 16), r);
+          const unsigned char* vrow = vtile(s_before);
+          const uint4 v0 = *reinterpret_cast<const uint4*>(vrow + sw128_offset(row, 4 * ch + 2 * p));
+          const uint4 v1 = *reinterpret_cast<const uint4*>(vrow + sw128_offset(row, 4 * ch + 2 * p + 1));
+          const uint32_t in[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+          tmem_wait_ld(y);
+          tmem_wait_ld(r);
+          uint32_t o[8];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t o[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int e = 8 * c + 2 * i;
-            const float2 z = fma2(unpack(xv[e / 2]), make_float2(skip, skip), fma2(make_float2(from_state, from_state), f2(r[e], r[e + 1]), f2(y[e], y[e + 1])));
+          for (int i = 0; i < 8; ++i) {
+            const float2 z = fma2(unpack(in[i]), sk, fma2(f, f2(r[2 * i], r[2 * i + 1]), f2(y[2 * i], y[2 * i + 1])));
             o[i] = dead ? 0u : pack_bf16(z.x, z.y);
           }
-          *reinterpret_cast<uint4*>(rows + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+          *reinterpret_cast<uint4*>(rows + lane * 64 + (((2 * p) ^ ((lane >> 1) & 3)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+          *reinterpret_cast<uint4*>(rows + lane * 64 + (((2 * p + 1) ^ ((lane >> 1) & 3)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
         }
+        tc_fence_before();
+        mbar_arrive(bars + BAR_O_EMPTY);
         fence_async_smem();
         __syncwarp();
         const int first = w.t0 + (j - 1) * CT + (int)q4 * 32;
-        if (lane == 0 && first < a.T) tma_store_4d(&tmO, rows, ch * 32, first, w.h, w.b);
-      }
-      if (j < w.tiles) {
-        from_state = from_here;
-        ok = warp_wait(bars + BAR_FULL + s, round & 1, abort_flag);
-        if (!ok) break;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) *reinterpret_cast<uint4*>(xv + 4 * c) = *reinterpret_cast<const uint4*>(vtile(s) + sw128_offset(row, ch * 4 + c));
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bars + BAR_EMPTY + s);
-        if (++s == NST) {
-          s = 0;
-          ++round;
+        if (lane == 0) {
+          mbar_arrive(bars + BAR_EMPTY + s_before);
+          if (first < a.T) tma_store_4d(&tmO, rows, ch * 32, first, w.h, w.b);
         }
+      }
+      from_state = from_here;
+      s_before = s;
+      if (++s == NST) {
+        s = 0;
+        ++round;
       }
     }
   }
@@ -623,17 +640,17 @@ tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     mma_commit(bars + BAR_DRAIN);
     mbar_wait(bars + BAR_DRAIN, 0);
   }
-  if (warp >= W_BLD0 && lane == 0) bulk_wait();
+  if (warp >= W_OUT0 && lane == 0) bulk_wait();
   __syncthreads();
   if (warp == 0) tmem_dealloc(tb, TMEM_COLS);
   // rows behind the last tile of the sequence
   const int first = w.t0 + w.tiles * CT;
-  for (long long i = tid; i < (long long)(w.t1 - first) * 8; i += NTHREADS)
+  for (long long i = tid; i < (long long)(w.t1 - first) * 8; i += kOutThreads)
     *reinterpret_cast<uint4*>(a.out + w.b * a.o0 + w.h * a.o1 + (first + (i >> 3)) * a.o2 + (i & 7) * 8) = make_uint4(0u, 0u, 0u, 0u);
 }
 
 template <int N>
-__global__ void __launch_bounds__(NTHREADS, 1)
+__global__ void __launch_bounds__(kStateThreads, 1)
 tc_ssm_state_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ Args a) {
   typedef Shape<N, true> Sh;
   constexpr int NST = Sh::NST;
@@ -681,7 +698,7 @@ tc_ssm_state_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
     if (lane == 0) {
       for (int j = 0; j < w.tiles && ok; ++j) {
         const int s = j % NST, tok = w.t0 + j * CT;
-        ok = wait_or_abort_counted(bars + BAR_EMPTY + s, ((j / NST) & 1) ^ 1, abort_flag);
+        ok = wait_or_abort(bars + BAR_EMPTY + s, ((j / NST) & 1) ^ 1, abort_flag);
         if (!ok) break;
         mbar_arrive_expect_tx(bars + BAR_FULL + s, Sh::STAGE);
 #pragma unroll
@@ -718,7 +735,7 @@ tc_ssm_state_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
     // =========================== decays ===========================
     const double all = decay_warp<false>(a, w, decays, bars, abort_flag, ok);
     if (lane == 0) a.decay[(size_t)w.bh * a.slots + w.seg] = ex2((float)all);
-  } else if (warp >= W_STATE0 && warp < W_BLD0) {
+  } else if (warp >= W_STATE0 && warp < W_WEIGHT0) {
     // =========================== state ===========================
     const int q4 = warp & 3, row = state_row<N>(q4, lane);
     float2 S[DV / 2];
@@ -750,9 +767,9 @@ tc_ssm_state_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
 #pragma unroll
       for (int c = 0; c < DV / 4; ++c) dst[c] = make_float4(S[2 * c].x, S[2 * c].y, S[2 * c + 1].x, S[2 * c + 1].y);
     }
-  } else if (warp >= W_BLD0) {
+  } else if (warp >= W_WEIGHT0) {
     // =========================== scaled V in three terms ===========================
-    const int q4 = warp & 3, ch = (warp - W_BLD0) >> 2, tok = q4 * 32 + lane;
+    const int q4 = warp & 3, ch = (warp - W_WEIGHT0) >> 2, tok = q4 * 32 + lane;
     for (int j = 0; j < w.tiles && ok; ++j) {
       const int s = j % NST, b = j & 1, slot = j & (NSLOT - 1);
       ok = warp_wait(bars + BAR_DEC_FULL + slot, (j / NSLOT) & 1, abort_flag);
@@ -832,11 +849,11 @@ template <int N> void launch(const Ssm& a, const SsmPlan& plan, float* ws, int* 
   if (states) {
     r.local = ws;
     r.decay = ws + (size_t)a.B * a.H * r.slots * (N * DV);
-    launch_after(ctx, tc_ssm_state_kernel<N>, grid, dim3(NTHREADS), Shape<N, true>::SMEM, tmK, tmV, r);
+    launch_after(ctx, tc_ssm_state_kernel<N>, grid, dim3(kStateThreads), Shape<N, true>::SMEM, tmK, tmV, r);
     ssm_prefix(a, plan, r.slots, ws, ctx);
     r.init = ws;
   }
-  launch_after(ctx, tc_ssm_out_kernel<N>, grid, dim3(NTHREADS), Shape<N, false>::SMEM, tmQ, tmK, tmV, tmO, r);
+  launch_after(ctx, tc_ssm_out_kernel<N>, grid, dim3(kOutThreads), Shape<N, false>::SMEM, tmQ, tmK, tmV, tmO, r);
 }
 
 }  // namespace
