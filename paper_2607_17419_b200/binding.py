@@ -152,7 +152,7 @@ class _CtypesOnly:
     def forward(*args):
         return NotImplemented
 
-    decode = backward = forward
+    decode = backward = norm_rope = norm_rope_bwd = short_conv = short_conv_bwd = ssm = forward
 
 
 def native():
@@ -633,10 +633,32 @@ def _mixer_call(name: str, args, q, fn: int = -1, sizes=(), *, workspace=None, s
 
 @functools.lru_cache(maxsize=64)
 def _frequencies(base: float, rotary_dim: int):
-    return (ctypes.c_double * max(1, rotary_dim // 2))(*(base ** (-2.0 * i / rotary_dim) for i in range(rotary_dim // 2)))
+    return tuple(float(base) ** (-2.0 * i / rotary_dim) for i in range(rotary_dim // 2))
 
 
-def _rope_args(q, k, q_weight, k_weight, positions, offset, base, inv_freq, rotary_dim, interleaved, eps):
+def _rope_freq(q, base, inv_freq, rotary_dim):
+    """The angles per position, a tuple or list of floats."""
+    if inv_freq is None:
+        if rotary_dim is None:
+            rotary_dim = q.shape[-1] if isinstance(q, torch.Tensor) and q.dim() > 0 else 0
+        return _frequencies(base, rotary_dim)
+    if isinstance(inv_freq, torch.Tensor):
+        if inv_freq.device.type != "cpu":
+            raise ValueError("inv_freq is a host sequence (it is read when the call is made)")
+        inv_freq = inv_freq.double().tolist()
+    if rotary_dim is not None and len(inv_freq) != rotary_dim // 2:
+        raise ValueError(f"inv_freq has {len(inv_freq)} entries, the call needs {rotary_dim // 2}")
+    return inv_freq
+
+
+def _native_result(name: str, r):
+    """What a native call gave, or NotImplemented where it is left to this file."""
+    if type(r) is int:
+        raise KataError(r, name)
+    return r
+
+
+def _rope_args(q, k, q_weight, k_weight, positions, offset, inv_freq, interleaved, eps):
     _want_main("q", q, 4)
     B, H, T, d = q.shape
     _want("q", q, q, q.shape)
@@ -649,19 +671,8 @@ def _rope_args(q, k, q_weight, k_weight, positions, offset, base, inv_freq, rota
     for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
         if w is not None:
             _want_contiguous(name, w, q, (d,))
-    if inv_freq is not None:
-        if isinstance(inv_freq, torch.Tensor):
-            if inv_freq.device.type != "cpu":
-                raise ValueError("inv_freq is a host sequence (it is read when the call is made)")
-            inv_freq = inv_freq.tolist()
-        if rotary_dim is None:
-            rotary_dim = 2 * len(inv_freq)
-        if len(inv_freq) != rotary_dim // 2:
-            raise ValueError(f"inv_freq has {len(inv_freq)} entries, the call needs {rotary_dim // 2}")
-        freq = (ctypes.c_double * max(1, len(inv_freq)))(*inv_freq)
-    else:
-        rotary_dim = d if rotary_dim is None else rotary_dim
-        freq = _frequencies(float(base), int(rotary_dim))
+    rotary_dim = 2 * len(inv_freq)
+    freq = (ctypes.c_double * max(1, len(inv_freq)))(*inv_freq)
     a = NormRopeArgs(B=B, T=T, H_q=H, H_k=k.shape[1] if k is not None else 0, d=d, rotary_dim=rotary_dim, interleaved=int(bool(interleaved)), eps=eps,
                      inv_freq=ctypes.addressof(freq), pos_offset=offset, q=q.data_ptr(), k=_ptr(k), q_weight=_ptr(q_weight), k_weight=_ptr(k_weight))
     a.freq = freq                                        # (held as long as the arguments)
@@ -684,7 +695,12 @@ def kata_fwd_norm_rope(q, k=None, q_weight=None, k_weight=None, positions=None, 
     rotation by the token's position (int64 [T] or [B,T], or offset + t).  q, k: any strides whose rows lie side by side, such as
     views of a projection.  inv_freq: angles per position, a host sequence of rotary_dim / 2 (else base^(-2i / rotary_dim)).
     Returns (q_out, k_out), contiguous [B,H,T,d] unless given."""
-    a = _rope_args(q, k, q_weight, k_weight, positions, offset, base, inv_freq, rotary_dim, interleaved, eps)
+    freq = _rope_freq(q, base, inv_freq, rotary_dim)
+    if stream is None:
+        r = _native_result("kata_fwd_norm_rope", (_native or native()).norm_rope(q, k, q_weight, k_weight, positions, offset, freq, interleaved, eps, q_out, k_out))
+        if r is not NotImplemented:
+            return r
+    a = _rope_args(q, k, q_weight, k_weight, positions, offset, freq, interleaved, eps)
     outs = []
     for name, x, out in (("q_out", q, q_out), ("k_out", k, k_out)):
         if x is None and out is not None:
@@ -706,7 +722,13 @@ def kata_bwd_norm_rope(dq_out, dk_out, q, k=None, q_weight=None, k_weight=None, 
                        workspace: Optional[Workspace] = None, stream=None):
     """Gradients of ``kata_fwd_norm_rope`` from those of its outputs: (dq, dk, dq_weight, dk_weight).  dq and dk take the layout of
     q and k unless given; the weights' gradients are fp32 [d] (None without a weight)."""
-    a = _rope_args(q, k, q_weight, k_weight, positions, offset, base, inv_freq, rotary_dim, interleaved, eps)
+    freq = _rope_freq(q, base, inv_freq, rotary_dim)
+    if workspace is None and stream is None:
+        r = _native_result("kata_bwd_norm_rope", (_native or native()).norm_rope_bwd(q, k, q_weight, k_weight, positions, offset, freq, interleaved, eps,
+                                                                                    _default_scratch, dq_out, dk_out, dq, dk))
+        if r is not NotImplemented:
+            return r
+    a = _rope_args(q, k, q_weight, k_weight, positions, offset, freq, interleaved, eps)
     grads, sums = [], []
     for name, x, g, dx, w in (("q", q, dq_out, dq, q_weight), ("k", k, dk_out, dk, k_weight)):
         if x is None:
@@ -757,6 +779,10 @@ def kata_fwd_short_conv(x, weight, bias=None, *, silu: bool = False, s_init=None
     """Causal convolution of x [B,T,D] along T with weight [D,width], bias [D] and optionally z * sigmoid(z).  s_init, s_final
     [B,D,width-1]: the inputs before the first and up to the last token (may be one tensor); lengths: int32 [B] of a padded
     batch.  Returns out [B,T,D], contiguous unless given."""
+    if stream is None and isinstance(x, torch.Tensor) and x.dim() == 3:
+        r = _native_result("kata_fwd_short_conv", (_native or native()).short_conv(x, weight, bias, silu, lengths, s_init, s_final, out))
+        if r is not NotImplemented:
+            return r
     a = _conv_args(x, weight, bias, silu, s_init, s_final, lengths)
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
@@ -770,6 +796,10 @@ def kata_fwd_short_conv(x, weight, bias=None, *, silu: bool = False, s_init=None
 
 def kata_decode_short_conv(x, weight, state, bias=None, *, silu: bool = False, out=None, stream=None):
     """One token of every sequence: x [B,D]; state [B,D,width-1] is moved on in place.  Returns out [B,D]."""
+    if stream is None and state is not None and isinstance(x, torch.Tensor) and x.dim() == 2:
+        r = _native_result("kata_decode_short_conv", (_native or native()).short_conv(x, weight, bias, silu, None, state, state, out))
+        if r is not NotImplemented:
+            return r
     _want_main("x", x, 2)
     a = _conv_args(x[:, None], weight, bias, silu, state, state, None)
     if state is None:
@@ -786,6 +816,10 @@ def kata_decode_short_conv(x, weight, state, bias=None, *, silu: bool = False, o
 
 def kata_bwd_short_conv(dout, x, weight, bias=None, *, silu: bool = False, lengths=None, dx=None, workspace: Optional[Workspace] = None, stream=None):
     """Gradients of ``kata_fwd_short_conv`` (without states): (dx, dweight [D,width] fp32, dbias [D] fp32 or None)."""
+    if workspace is None and stream is None:
+        r = _native_result("kata_bwd_short_conv", (_native or native()).short_conv_bwd(x, weight, bias, silu, lengths, _default_scratch, dout, dx))
+        if r is not NotImplemented:
+            return r
     a = _conv_args(x, weight, bias, silu, None, None, lengths)
     _want("dout", dout, x, x.shape)
     if dx is None:
@@ -835,6 +869,10 @@ def kata_fwd_ssm_scan(q, k, v, dt, A, D=None, dt_bias=None, *, dt_softplus: bool
     softplus).  q, k [B,G,T,n]; v [B,H,T,d_v]; dt [B,H,T]; A, D, dt_bias [H] fp32; s_init, s_final [B,H,n,d_v] fp32, the states
     before the first and after the last token (may be one tensor); lengths: int32 [B] of a padded batch.  Strided views are
     taken as they are; out takes the layout of v unless given."""
+    if workspace is None and stream is None and device_status is None and isinstance(v, torch.Tensor) and v.dim() == 4:
+        r = _native_result("kata_fwd_ssm_scan", (_native or native()).ssm(_default_scratch, q, k, v, dt, A, D, dt_bias, dt_softplus, s_init, s_final, lengths, out, impl))
+        if r is not NotImplemented:
+            return r
     a, out = _ssm_args(q, k, v, dt, A, D, dt_bias, dt_softplus, lengths, out)
     for name, s in (("s_init", s_init), ("s_final", s_final)):
         if s is not None:
@@ -848,6 +886,10 @@ def kata_fwd_ssm_scan(q, k, v, dt, A, D=None, dt_bias=None, *, dt_softplus: bool
 def kata_decode_ssm_step(q, k, v, dt, A, state, D=None, dt_bias=None, *, dt_softplus: bool = False, out=None, stream=None):
     """One token of the scan for every head: q, k [B,G,n]; v [B,H,d_v]; dt [B,H]; state [B,H,n,d_v] fp32 is moved on in place.
     Returns out [B,H,d_v]."""
+    if stream is None and state is not None and isinstance(v, torch.Tensor) and v.dim() == 3:
+        r = _native_result("kata_decode_ssm_step", (_native or native()).ssm(None, q, k, v, dt, A, D, dt_bias, dt_softplus, state, state, None, out, KATA_IMPL_AUTO))
+        if r is not NotImplemented:
+            return r
     for name, x, dim in (("q", q, 3), ("k", k, 3), ("v", v, 3), ("dt", dt, 2)):
         if not isinstance(x, torch.Tensor) or x.dim() != dim:
             raise ValueError(f"{name} must be a tensor of {dim} axes")

@@ -62,9 +62,9 @@ int norm_rope(const kata_norm_rope_args* a, const kata_opts* opts, bool backward
   for (int i = 0; i < a->rotary_dim / 2; ++i) {
     if (!std::isfinite(a->inv_freq[i])) return KATA_ERR_INVALID_ARG;
     // turns a position: a fraction of 2^64 (whole turns do not count), to the 64 bits of a long double
-    long double turn = (long double)a->inv_freq[i] / 6.283185307179586476925286766559005768L;
-    turn -= floorl(turn);
-    const long double scaled = roundl(turn * 18446744073709551616.0L);
+    long double turn = (long double)a->inv_freq[i] * (1.0L / 6.283185307179586476925286766559005768L);
+    if (!(turn >= 0.0L && turn < 1.0L)) turn -= floorl(turn);
+    const long double scaled = turn * 18446744073709551616.0L + 0.5L;
     r.turns[i] = scaled >= 18446744073709551616.0L ? 0ull : (unsigned long long)scaled;
   }
   struct Tensor { View* to; const void* p; const int64_t* stride; int heads; bool output; };

@@ -8,7 +8,9 @@
 #include <Python.h>
 
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <cuda_runtime_api.h>
 #include <torch/csrc/Exceptions.h>
@@ -284,10 +286,301 @@ PyObject* backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-PyMethodDef kMethods[] = {{"forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(forward)), METH_FASTCALL, nullptr},
-                          {"decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(decode)), METH_FASTCALL, nullptr},
-                          {"backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(backward)), METH_FASTCALL, nullptr},
-                          {nullptr, nullptr, 0, nullptr}};
+// ---- rows around the attention and the decayed recurrence (binding.py: the functions of the same names) ----
+// Strided views whose rows lie side by side, on the current device; everything else is left to binding.py.
+
+// The tensor if it is plain, has these sizes and this type, and lies on main's device (main: itself).
+const at::Tensor* view(PyObject* o, const at::Tensor* main, std::initializer_list<int64_t> sizes, at::ScalarType type, bool contiguous = false) {
+  const at::Tensor* t = plain(o);
+  if (t == nullptr || t->scalar_type() != type || t->dim() != (int64_t)sizes.size() || (main != nullptr && t->device() != main->device())) return nullptr;
+  int64_t i = 0;
+  for (int64_t n : sizes)
+    if (t->size(i++) != n) return nullptr;
+  if (contiguous) return t->is_contiguous() ? t : nullptr;
+  return t->size(-1) == 1 || t->stride(-1) == 1 ? t : nullptr;
+}
+bool main_tensor(PyObject* o, int64_t dim, const at::Tensor*& t, kata_opts& opts) {
+  t = plain(o);
+  opts = kata_opts{};
+  opts.struct_size = sizeof(kata_opts);
+  if (t == nullptr || t->dim() != dim || !dtype_code(*t, opts.dtype) || t->numel() == 0 || t->device().index() != c10::cuda::current_device()) return false;
+  for (int64_t i = 0; i < dim; ++i)
+    if (t->size(i) > INT_MAX) return false;
+  return t->size(-1) == 1 || t->stride(-1) == 1;
+}
+// An optional contiguous tensor's pointer; false: one that is left to binding.py.
+template <typename T> bool optional(PyObject* o, const at::Tensor& main, std::initializer_list<int64_t> sizes, at::ScalarType type, T*& p) {
+  p = nullptr;
+  if (o == Py_None) return true;
+  const at::Tensor* t = view(o, &main, sizes, type, true);
+  if (t == nullptr) return false;
+  p = static_cast<T*>(const_cast<void*>(static_cast<const void*>(t->data_ptr())));
+  return true;
+}
+void strides(const at::Tensor& t, int64_t* to, int n) {
+  for (int i = 0; i < n; ++i) to[i] = t.stride(i);
+}
+at::Tensor make_output(PyObject* o, const at::Tensor& like, bool same_layout) {
+  return o != Py_None ? THPVariable_Unpack(o) : same_layout ? at::empty_like(like) : at::empty(like.sizes(), like.options());
+}
+bool given_fits(PyObject* o, const at::Tensor& like) {
+  if (o == Py_None) return true;
+  const at::Tensor* t = plain(o);
+  return t != nullptr && t->sizes() == like.sizes() && t->scalar_type() == like.scalar_type() && t->device() == like.device() &&
+         (t->size(-1) == 1 || t->stride(-1) == 1);
+}
+PyObject* tuple_of(int status, std::initializer_list<const at::Tensor*> out) {
+  if (status != KATA_OK) return PyLong_FromLong(status);
+  PyObject* tuple = PyTuple_New((Py_ssize_t)out.size());
+  Py_ssize_t i = 0;
+  for (const at::Tensor* t : out) {
+    PyObject* x = tuple == nullptr ? nullptr : t->defined() ? THPVariable_Wrap(*t) : (Py_INCREF(Py_None), Py_None);
+    if (x == nullptr) {
+      Py_XDECREF(tuple);
+      return nullptr;
+    }
+    PyTuple_SET_ITEM(tuple, i++, x);
+  }
+  return tuple;
+}
+
+// q, k, q_weight, k_weight, positions, offset, frequencies (tuple or list of floats), interleaved, eps: the arguments of both calls
+bool rope_args(PyObject* const* a, kata_norm_rope_args& r, double (&freq)[64], kata_opts& o, const at::Tensor*& q, const at::Tensor*& k) {
+  if (at::impl::torch_function_mode_enabled() || !main_tensor(a[0], 4, q, o)) return false;
+  r = kata_norm_rope_args{};
+  r.struct_size = sizeof r;
+  r.B = (int)q->size(0); r.H_q = (int)q->size(1); r.T = (int)q->size(2); r.d = (int)q->size(3);
+  k = nullptr;
+  if (a[1] != Py_None) {
+    const at::Tensor* t = plain(a[1]);
+    if (t == nullptr || t->dim() != 4 || t->size(1) > INT_MAX) return false;
+    k = view(a[1], q, {r.B, t->size(1), r.T, r.d}, q->scalar_type());
+    if (k == nullptr) return false;
+    r.H_k = (int)k->size(1);
+  } else if (a[3] != Py_None) {
+    return false;
+  }
+  if (!optional(a[2], *q, {r.d}, q->scalar_type(), r.q_weight) || !optional(a[3], *q, {r.d}, q->scalar_type(), r.k_weight)) return false;
+  if (a[4] != Py_None) {
+    const at::Tensor* p = plain(a[4]);
+    if (p == nullptr || p->scalar_type() != at::kLong || p->device() != q->device() || p->dim() < 1 || p->dim() > 2 || p->size(-1) != r.T ||
+        (p->dim() == 2 && p->size(0) != r.B))
+      return false;
+    r.positions = p->data_ptr<int64_t>();
+    r.pos_stride[0] = p->dim() == 2 ? p->stride(0) : 0;
+    r.pos_stride[1] = p->stride(-1);
+  }
+  int overflow = 0;
+  if (!PyLong_CheckExact(a[5])) return false;
+  r.pos_offset = PyLong_AsLongLongAndOverflow(a[5], &overflow);
+  if (overflow != 0 || !(PyTuple_CheckExact(a[6]) || PyList_CheckExact(a[6])) || !PyFloat_CheckExact(a[8])) return false;
+  const Py_ssize_t n = PySequence_Fast_GET_SIZE(a[6]);
+  if (n > 64) return false;
+  PyObject** items = PySequence_Fast_ITEMS(a[6]);
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    if (!PyFloat_CheckExact(items[i])) return false;
+    freq[i] = PyFloat_AS_DOUBLE(items[i]);
+  }
+  r.inv_freq = freq;
+  r.rotary_dim = (int)(2 * n);
+  r.interleaved = PyObject_IsTrue(a[7]) == 1;
+  r.eps = PyFloat_AS_DOUBLE(a[8]);
+  r.q = q->data_ptr();
+  strides(*q, r.q_stride, 3);
+  if (k != nullptr) {
+    r.k = k->data_ptr();
+    strides(*k, r.k_stride, 3);
+  }
+  return true;
+}
+
+// norm_rope(q, k, q_weight, k_weight, positions, offset, frequencies, interleaved, eps, q_out, k_out)
+PyObject* norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  kata_norm_rope_args r;
+  kata_opts o;
+  double freq[64];
+  const at::Tensor *q, *k;
+  if (n != 11 || !rope_args(a, r, freq, o, q, k) || !given_fits(a[9], *q) || (k == nullptr ? a[10] != Py_None : !given_fits(a[10], *k))) return not_implemented();
+  const at::Tensor qo = make_output(a[9], *q, false), ko = k != nullptr ? make_output(a[10], *k, false) : at::Tensor();
+  r.q_out = qo.data_ptr();
+  strides(qo, r.q_out_stride, 3);
+  if (k != nullptr) {
+    r.k_out = ko.data_ptr();
+    strides(ko, r.k_out_stride, 3);
+  }
+  o.stream = c10::cuda::getCurrentCUDAStream(q->device().index()).stream();
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = kata_fwd_norm_rope(&r, &o);
+  Py_END_ALLOW_THREADS
+  return tuple_of(st, {&qo, &ko});
+  END_HANDLE_TH_ERRORS
+}
+
+// norm_rope_bwd(q, k, q_weight, k_weight, positions, offset, frequencies, interleaved, eps, scratch owner, dq_out, dk_out, dq, dk)
+PyObject* norm_rope_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  kata_norm_rope_args r;
+  kata_opts o;
+  double freq[64];
+  const at::Tensor *q, *k;
+  if (n != 14 || !rope_args(a, r, freq, o, q, k) || a[10] == Py_None || !given_fits(a[10], *q) || !given_fits(a[12], *q)) return not_implemented();
+  if (k == nullptr ? a[11] != Py_None || a[13] != Py_None : a[11] == Py_None || !given_fits(a[11], *k) || !given_fits(a[13], *k)) return not_implemented();
+  PyObject* held;
+  if (!stream_and_scratch(a[9], *q, KATA_FN_BWD_NORM_ROPE, r.B, r.H_q + r.H_k, r.T, r.d, 0, 0, o, held)) return not_implemented();
+  const Held hold{held};
+  const at::Tensor &go = THPVariable_Unpack(a[10]), dq = make_output(a[12], *q, true);
+  at::Tensor dk, dqw, dkw;
+  r.q_out = go.data_ptr();
+  strides(go, r.q_out_stride, 3);
+  r.dq = dq.data_ptr();
+  strides(dq, r.dq_stride, 3);
+  if (r.q_weight != nullptr) {
+    dqw = at::empty({r.d}, q->options().dtype(at::kFloat));
+    r.dq_weight = dqw.data_ptr<float>();
+  }
+  if (k != nullptr) {
+    const at::Tensor& gk = THPVariable_Unpack(a[11]);
+    dk = make_output(a[13], *k, true);
+    r.k_out = gk.data_ptr();
+    strides(gk, r.k_out_stride, 3);
+    r.dk = dk.data_ptr();
+    strides(dk, r.dk_stride, 3);
+    if (r.k_weight != nullptr) {
+      dkw = at::empty({r.d}, q->options().dtype(at::kFloat));
+      r.dk_weight = dkw.data_ptr<float>();
+    }
+  }
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = kata_bwd_norm_rope(&r, &o);
+  Py_END_ALLOW_THREADS
+  return tuple_of(st, {&dq, &dk, &dqw, &dkw});
+  END_HANDLE_TH_ERRORS
+}
+
+// x, weight, bias, silu, lengths: the arguments of the three calls; `dim`: axes of x (2: one token)
+bool conv_args(PyObject* const* a, int64_t dim, kata_short_conv_args& r, kata_opts& o, const at::Tensor*& x, const at::Tensor*& w) {
+  if (at::impl::torch_function_mode_enabled() || !main_tensor(a[0], dim, x, o)) return false;
+  r = kata_short_conv_args{};
+  r.struct_size = sizeof r;
+  r.B = (int)x->size(0); r.T = dim == 3 ? (int)x->size(1) : 1; r.D = (int)x->size(-1);
+  const at::Tensor* t = plain(a[1]);
+  if (t == nullptr || t->dim() != 2 || t->size(1) > INT_MAX) return false;
+  w = view(a[1], x, {r.D, t->size(1)}, x->scalar_type(), true);
+  if (w == nullptr) return false;
+  r.width = (int)w->size(1);
+  r.weight = w->data_ptr();
+  if (!optional(a[2], *x, {r.D}, x->scalar_type(), r.bias) || !optional(a[4], *x, {r.B}, at::kInt, r.lengths)) return false;
+  r.silu = PyObject_IsTrue(a[3]) == 1;
+  r.x = x->data_ptr();
+  strides(*x, r.x_stride, (int)dim - 1);
+  return true;
+}
+
+// short_conv(x, weight, bias, silu, lengths, s_init, s_final, out); x of two axes: one token
+PyObject* short_conv(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  kata_short_conv_args r;
+  kata_opts o;
+  const at::Tensor *x, *w;
+  if (n != 8 || !THPVariable_CheckExact(a[0])) return not_implemented();
+  const int64_t dim = THPVariable_Unpack(a[0]).dim();
+  if ((dim != 2 && dim != 3) || !conv_args(a, dim, r, o, x, w) || !given_fits(a[7], *x)) return not_implemented();
+  if (!optional(a[5], *x, {r.B, r.D, r.width - 1}, x->scalar_type(), r.s_init) || !optional(a[6], *x, {r.B, r.D, r.width - 1}, x->scalar_type(), r.s_final))
+    return not_implemented();
+  const at::Tensor out = make_output(a[7], *x, false);
+  r.out = out.data_ptr();
+  strides(out, r.out_stride, (int)dim - 1);
+  o.stream = c10::cuda::getCurrentCUDAStream(x->device().index()).stream();
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = dim == 2 ? kata_decode_short_conv(&r, &o) : kata_fwd_short_conv(&r, &o);
+  Py_END_ALLOW_THREADS
+  return result(st, {&out});
+  END_HANDLE_TH_ERRORS
+}
+
+// short_conv_bwd(x, weight, bias, silu, lengths, scratch owner, dout, dx)
+PyObject* short_conv_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  kata_short_conv_args r;
+  kata_opts o;
+  const at::Tensor *x, *w;
+  if (n != 8 || !conv_args(a, 3, r, o, x, w) || a[6] == Py_None || !given_fits(a[6], *x) || !given_fits(a[7], *x)) return not_implemented();
+  PyObject* held;
+  if (!stream_and_scratch(a[5], *x, KATA_FN_BWD_SHORT_CONV, r.B, r.D, r.T, r.width, 0, 0, o, held)) return not_implemented();
+  const Held hold{held};
+  const at::Tensor &g = THPVariable_Unpack(a[6]), dx = make_output(a[7], *x, false), dw = at::empty(w->sizes(), w->options().dtype(at::kFloat)),
+                   db = r.bias != nullptr ? at::empty({r.D}, w->options().dtype(at::kFloat)) : at::Tensor();
+  r.dout = g.data_ptr();
+  strides(g, r.dout_stride, 2);
+  r.dx = dx.data_ptr();
+  strides(dx, r.dx_stride, 2);
+  r.dweight = dw.data_ptr<float>();
+  r.dbias = db.defined() ? db.data_ptr<float>() : nullptr;
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = kata_bwd_short_conv(&r, &o);
+  Py_END_ALLOW_THREADS
+  return tuple_of(st, {&dx, &dw, &db});
+  END_HANDLE_TH_ERRORS
+}
+
+// ssm(scratch owner, q, k, v, dt, A, D, dt_bias, dt_softplus, s_init, s_final, lengths, out, impl); v of three axes: one token
+PyObject* ssm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  kata_opts o;
+  const at::Tensor *v, *q, *k, *dt;
+  if (n != 14 || !THPVariable_CheckExact(a[3]) || !PyLong_CheckExact(a[13]) || at::impl::torch_function_mode_enabled()) return not_implemented();
+  const int64_t dim = THPVariable_Unpack(a[3]).dim();
+  if ((dim != 3 && dim != 4) || !main_tensor(a[3], dim, v, o)) return not_implemented();
+  const bool step = dim == 3;
+  q = plain(a[1]);
+  if (q == nullptr || q->dim() != dim || q->size(1) > INT_MAX || q->size(-1) > INT_MAX) return not_implemented();
+  kata_ssm_args r{};
+  r.struct_size = sizeof r;
+  r.B = (int)v->size(0); r.H = (int)v->size(1); r.T = step ? 1 : (int)v->size(2); r.d_v = (int)v->size(-1);
+  r.G = (int)q->size(1); r.n = (int)q->size(-1);
+  const at::ScalarType type = v->scalar_type();
+  q = step ? view(a[1], v, {r.B, r.G, r.n}, type) : view(a[1], v, {r.B, r.G, r.T, r.n}, type);
+  k = step ? view(a[2], v, {r.B, r.G, r.n}, type) : view(a[2], v, {r.B, r.G, r.T, r.n}, type);
+  dt = plain(a[4]);
+  if (q == nullptr || k == nullptr || dt == nullptr || dt->dim() != dim - 1 || dt->scalar_type() != type || dt->device() != v->device() || dt->size(0) != r.B ||
+      dt->size(1) != r.H || (!step && dt->size(2) != r.T))
+    return not_implemented();
+  if (a[5] == Py_None || !optional(a[5], *v, {r.H}, at::kFloat, r.A) || !optional(a[6], *v, {r.H}, at::kFloat, r.D) ||
+      !optional(a[7], *v, {r.H}, at::kFloat, r.dt_bias) || !optional(a[9], *v, {r.B, r.H, r.n, r.d_v}, at::kFloat, r.s_init) ||
+      !optional(a[10], *v, {r.B, r.H, r.n, r.d_v}, at::kFloat, r.s_final) || !optional(a[11], *v, {r.B}, at::kInt, r.lengths) || !given_fits(a[12], *v))
+    return not_implemented();
+  r.dt_softplus = PyObject_IsTrue(a[8]) == 1;
+  const long impl = PyLong_AsLong(a[13]);
+  if (impl < INT_MIN || impl > INT_MAX) return not_implemented();
+  o.impl = (int)impl;
+  PyObject* held = nullptr;
+  if (step) o.stream = c10::cuda::getCurrentCUDAStream(v->device().index()).stream();
+  else if (!stream_and_scratch(a[0], *v, KATA_FN_SSM_SCAN, r.B, r.H, r.T, r.n, r.d_v, 0, o, held)) return not_implemented();
+  const Held hold{held};
+  const at::Tensor out = make_output(a[12], *v, true);
+  r.q = q->data_ptr(); r.k = k->data_ptr(); r.v = v->data_ptr(); r.dt = dt->data_ptr(); r.out = out.data_ptr();
+  const int axes = (int)dim - 1;
+  strides(*q, r.q_stride, axes);
+  strides(*k, r.k_stride, axes);
+  strides(*v, r.v_stride, axes);
+  strides(*dt, r.dt_stride, axes);
+  strides(out, r.out_stride, axes);
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = step ? kata_decode_ssm_step(&r, &o) : kata_fwd_ssm_scan(&r, &o);
+  Py_END_ALLOW_THREADS
+  return result(st, {&out});
+  END_HANDLE_TH_ERRORS
+}
+
+#define KATA_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
+PyMethodDef kMethods[] = {KATA_METHOD(forward),        KATA_METHOD(decode),         KATA_METHOD(backward), KATA_METHOD(norm_rope), KATA_METHOD(norm_rope_bwd),
+                          KATA_METHOD(short_conv),     KATA_METHOD(short_conv_bwd), KATA_METHOD(ssm),      {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_kata_torch", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
