@@ -204,6 +204,22 @@ __device__ __forceinline__ double decay_warp(const Args& a, const Where& w, Deca
       if ((lane & 7) >= off) upto += o;
     }
     const float base = upto - sum, mine = __shfl_sync(0xffffffffu, upto, 7, 8);     // before this lane's tokens; of the whole block
+    // What a token loses up to the end of its block, summed from the end: as a difference it would carry the rounding of the whole
+    // block's sum, 2^-19 of the weight where the block decays by 2^-50.
+    float after = 0.f, lost[4];
+#pragma unroll
+    for (int i = 3; i >= 0; --i) {
+      lost[i] = after;
+      after = fmaf(s[i], rate, after);
+    }
+    float from = after;
+#pragma unroll
+    for (int off = 1; off < 8; off <<= 1) {
+      const float o = __shfl_down_sync(0xffffffffu, from, off, 8);
+      if ((lane & 7) + off < 8) from += o;
+    }
+    from = __shfl_down_sync(0xffffffffu, from, 1, 8);
+    if ((lane & 7) == 7) from = 0.f;
     const float b0 = __shfl_sync(0xffffffffu, mine, 0), b1 = __shfl_sync(0xffffffffu, mine, 8), b2 = __shfl_sync(0xffffffffu, mine, 16),
                 b3 = __shfl_sync(0xffffffffu, mine, 24);
     all += (double)b0 + b1 + b2 + b3;
@@ -216,7 +232,7 @@ __device__ __forceinline__ double decay_warp(const Args& a, const Where& w, Deca
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       c[i] += base;
-      tail[i] = s[i] * ex2(mine - c[i]);
+      tail[i] = s[i] * ex2(from + lost[i]);
     }
     reinterpret_cast<float4*>(d.left)[lane] = make_float4(tail[0] * behind, tail[1] * behind, tail[2] * behind, tail[3] * behind);
     if (ALL) {
