@@ -48,7 +48,7 @@ int norm_rope(const kata_norm_rope_args* a, const kata_opts* opts, bool backward
   if (a->B < 1 || a->T < 1 || a->H_q < 1 || a->H_k < 0 || a->d < 1 || a->rotary_dim < 0) return KATA_ERR_INVALID_ARG;
   if (!rope_width(a->d) || a->rotary_dim > a->d || a->rotary_dim % 16 != 0) return KATA_ERR_UNSUPPORTED_SHAPE;
   // (a row has at most 32 lanes, and the grid's axes are 32-bit)
-  if (a->H_q > 65535 || a->H_k > 65535 || (long long)a->B * a->T > (1LL << 31)) return KATA_ERR_UNSUPPORTED_SHAPE;
+  if (a->H_q > 32767 || a->H_k > 32767 || (long long)a->B * a->T > (1LL << 31) - 1024) return KATA_ERR_UNSUPPORTED_SHAPE;
   if (o.impl == KATA_IMPL_TENSOR) return KATA_ERR_UNSUPPORTED_SHAPE;
   if (!(a->eps >= 0.0) || !std::isfinite(a->eps) || (a->rotary_dim > 0 && a->inv_freq == nullptr)) return KATA_ERR_INVALID_ARG;
   NormRope r = {};

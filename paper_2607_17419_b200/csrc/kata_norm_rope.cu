@@ -2,9 +2,11 @@
 //   y = R_p (w * x r),  r = 1 / sqrt(mean(x^2) + eps)
 //   u = R_p^T dy,  dw = sum u * x r,  dx = r (u * w - x r mean(u * w * x r))
 // HBM-bound: every row is read and written once (backward: two reads, one write).  A row is held by d / (16 bytes) neighbouring
-// lanes, 16 bytes each.  The turn of a pair depends on the token and not on the head, so the lanes of a token form their sines
-// once and walk the heads with them.  An entry of the result is r (x c + x' s) with x' the other entry of its pair, c = cos w and
-// s = -+ sin w': the pair's raw 16 bytes come from their lane by four shuffles.
+// lanes.  A lane has both sides of its pairs, as two pieces of 8 bytes, so nothing but the sums of a row crosses lanes.  The turn of
+// a pair depends on the token and not on the head: the lanes of a token form their sines once and walk the heads with them.
+// Arithmetic goes two entries at a time.  Bound by latency more than by bandwidth: 8 x 4096 tokens, 32 heads of 64 in bf16, forward
+// and backward 161 us for 671 MB (three blocks of the backward and four of the forward on an SM; two and three: 181; one head in
+// flight less each: 164).
 // Angles: position times a 64-bit fraction of a turn, in wrapping integers: no rounding grows with the position.
 #include "kata_rows.cuh"
 
@@ -12,108 +14,184 @@ namespace kata {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kAhead = 4;                // heads in flight
-constexpr int kMaxBwdBlocks = 4 * kPlanSMs;
+constexpr int kAhead = 4, kBwdAhead = 2;                   // heads in flight
+constexpr int kBlocks = 3 * kPlanSMs;                      // of the backward: what fits at once
 
-// cos and +-sin of this lane's entries at a position (the sign of the entry's side of the pair: y = x cos + x' sin).
-template <int E, bool NEIGHBOURS>
-__device__ __forceinline__ void turns_of(const NormRope& a, const unsigned long long* turns, int e0, long long pos, float (&c)[E], float (&s)[E]) {
-  const int half = a.rot / 2;
+// What a lane has of a row: entries e0 .. and e1 .. (N pairs of entries each).  Of half-split pairs e1 holds the other sides; of
+// neighbouring ones the even entries of both pieces are one side.  Entries that are not turned fill the lanes behind.
+template <typename T> struct Half {
+  static constexpr int E = 8 / sizeof(T), N = E / 2;       // entries of a piece, pairs of them
+};
+struct Lane {
+  int e0, e1;
+  bool turned;
+};
+template <typename T, bool NEIGHBOURS>
+__device__ __forceinline__ Lane lane_of(const NormRope& a, int lanes) {
+  constexpr int E = Half<T>::E;
+  const int l = threadIdx.x & (lanes - 1), turning = a.rot / (2 * E);
+  Lane r;
+  r.turned = l < turning;
+  r.e0 = NEIGHBOURS || !r.turned ? 2 * E * l : E * l;
+  r.e1 = NEIGHBOURS || !r.turned ? r.e0 + E : a.rot / 2 + E * l;
+  return r;
+}
+
+// The two sides of a lane's pairs, as fp32 in twos.
+template <typename T> struct Sides {
+  static constexpr int N = Half<T>::N;
+  float2 a[N], b[N];
+};
+template <typename T> struct Pieces {
+  Entries<T, Half<T>::E> p, q;
+  __device__ __forceinline__ void load(const T* row, const Lane& ln) {
+    p.load(row + ln.e0);
+    q.load(row + ln.e1);
+  }
+  __device__ __forceinline__ void store(T* row, const Lane& ln) const {
+    p.store(row + ln.e0);
+    q.store(row + ln.e1);
+  }
+  __device__ __forceinline__ void zero() {
+    p.zero();
+    q.zero();
+  }
+  template <bool NEIGHBOURS> __device__ __forceinline__ Sides<T> get() const {
+    constexpr int E = Half<T>::E, N = Half<T>::N;
+    float x[E], y[E];
+    p.get(x);
+    q.get(y);
+    Sides<T> s;
 #pragma unroll
-  for (int j = 0; j < E; ++j) {
-    const int i = e0 + j;
-    c[j] = 1.f;
-    s[j] = 0.f;
-    if (i < a.rot) {
-      if (NEIGHBOURS && (j & 1)) {
-        c[j] = c[j - 1];
-        s[j] = -s[j - 1];
+    for (int i = 0; i < N; ++i) {
+      if (NEIGHBOURS) {                                    // pairs (x0 x1) (x2 x3) .. (y0 y1) ..
+        const int j = 4 * i;
+        s.a[i] = make_float2(j < E ? x[j < E ? j : 0] : y[j < E ? 0 : j - E], j + 2 < E ? x[j + 2 < E ? j + 2 : 0] : y[j + 2 < E ? 0 : j + 2 - E]);
+        s.b[i] = make_float2(j < E ? x[j < E ? j + 1 : 0] : y[j < E ? 0 : j + 1 - E], j + 2 < E ? x[j + 2 < E ? j + 3 : 0] : y[j + 2 < E ? 0 : j + 3 - E]);
       } else {
-        const int f = NEIGHBOURS ? i / 2 : (i < half ? i : i - half);
-        const unsigned long long turn = (unsigned long long)pos * turns[f];
-        float sn;
-        sincospif((float)(int)(turn >> 32) * 4.656612873077392578125e-10f, &sn, &c[j]);     // half turns in [-1, 1)
-        s[j] = NEIGHBOURS || i < half ? -sn : sn;
+        s.a[i] = make_float2(x[2 * i], x[2 * i + 1]);
+        s.b[i] = make_float2(y[2 * i], y[2 * i + 1]);
       }
+    }
+    return s;
+  }
+  template <bool NEIGHBOURS> __device__ __forceinline__ void set(const Sides<T>& s) {
+    constexpr int E = Half<T>::E, N = Half<T>::N;
+    float x[E], y[E];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (NEIGHBOURS) {
+        const int j = 4 * i;
+        const float v[4] = {s.a[i].x, s.b[i].x, s.a[i].y, s.b[i].y};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (j + k < E) x[j + k < E ? j + k : 0] = v[k];
+          else y[j + k < E ? 0 : j + k - E] = v[k];
+      } else {
+        x[2 * i] = s.a[i].x;
+        x[2 * i + 1] = s.a[i].y;
+        y[2 * i] = s.b[i].x;
+        y[2 * i + 1] = s.b[i].y;
+      }
+    }
+    p.set(x);
+    q.set(y);
+  }
+};
+
+// cos and sin of this lane's pairs at a position.
+template <typename T, bool NEIGHBOURS>
+__device__ __forceinline__ void turns_of(const unsigned long long* turns, const Lane& ln, long long pos, float2 (&c)[Half<T>::N], float2 (&s)[Half<T>::N]) {
+  const int f = NEIGHBOURS ? ln.e0 / 2 : ln.e0;            // first pair
+#pragma unroll
+  for (int i = 0; i < Half<T>::N; ++i) {
+    c[i] = make_float2(1.f, 1.f);
+    s[i] = make_float2(0.f, 0.f);
+    if (ln.turned) {
+      // half turns in [-1, 1)
+      sincospif((float)(int)(((unsigned long long)pos * turns[f + 2 * i]) >> 32) * 4.656612873077392578125e-10f, &s[i].x, &c[i].x);
+      sincospif((float)(int)(((unsigned long long)pos * turns[f + 2 * i + 1]) >> 32) * 4.656612873077392578125e-10f, &s[i].y, &c[i].y);
     }
   }
 }
 
-// The raw entries of the other side of the pairs.
-template <typename T, int E, bool NEIGHBOURS>
-__device__ __forceinline__ void partner(const Entries<T, E>& x, int src, float (&out)[E]) {
-  if (NEIGHBOURS) {
-    float v[E];
-    x.get(v);
+template <typename T, bool NEIGHBOURS>
+__device__ __forceinline__ Sides<T> weights_of(const void* w, const Lane& ln) {
+  constexpr int E = Half<T>::E;
+  Sides<T> r;
+  Pieces<T> x;
+  float one[E];
 #pragma unroll
-    for (int j = 0; j < E; ++j) out[j] = v[j ^ 1];
-  } else {
-    Entries<T, E> y;
-    y.raw.x = __shfl_sync(0xffffffffu, x.raw.x, src);
-    y.raw.y = __shfl_sync(0xffffffffu, x.raw.y, src);
-    y.raw.z = __shfl_sync(0xffffffffu, x.raw.z, src);
-    y.raw.w = __shfl_sync(0xffffffffu, x.raw.w, src);
-    y.get(out);
+  for (int i = 0; i < E; ++i) one[i] = 1.f;
+  x.p.set(one);
+  x.q.set(one);
+  if (w != nullptr) {                                      // (entry by entry: weights have no alignment to keep)
+    float u[E], v[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      u[i] = to_f32<T>(static_cast<const T*>(w)[ln.e0 + i]);
+      v[i] = to_f32<T>(static_cast<const T*>(w)[ln.e1 + i]);
+    }
+    x.p.set(u);
+    x.q.set(v);
   }
+  return x.template get<NEIGHBOURS>();
 }
 
-struct Lane {
-  int e0, src;                            // first entry, lane of the other side of its pairs
-};
-template <int E>
-__device__ __forceinline__ Lane lane_of(const NormRope& a, int lanes) {
-  const int lane = threadIdx.x & 31, l = lane & (lanes - 1), half = a.rot / 2 / E;        // (of half-split pairs)
-  Lane r;
-  r.e0 = l * E;
-  r.src = l < half ? lane + half : l < 2 * half ? lane - half : lane;
-  return r;
+__device__ __forceinline__ float2 twice(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float row_sum(float x, int lanes) {
+  for (int m = lanes >> 1; m > 0; m >>= 1) x += __shfl_xor_sync(0xffffffffu, x, m);
+  return x;
 }
 
-template <typename T, int E>
-__device__ __forceinline__ void load_weight(const void* w, int e0, float (&out)[E]) {
-#pragma unroll
-  for (int j = 0; j < E; ++j) out[j] = w != nullptr ? to_f32<T>(static_cast<const T*>(w)[e0 + j]) : 1.f;
-}
-
-template <typename T, int E, bool NEIGHBOURS>
+template <typename T, bool NEIGHBOURS>
 __device__ __forceinline__ void forward_heads(const NormRope& a, const View& in, const View& out, const void* weight, long long b, long long t,
-                                              int h0, int h1, bool on, const Lane& ln, int lanes, const float (&c)[E], const float (&s)[E]) {
-  float cw[E], sw[E], w[E];
-  load_weight<T, E>(weight, ln.e0, w);
-  const int half = a.rot / 2, e1 = ln.e0 < half ? ln.e0 + half : ln.e0 - half;
+                                              int h0, int h1, bool on, const Lane& ln, int lanes, const float2 (&c)[Half<T>::N], const float2 (&s)[Half<T>::N]) {
+  constexpr int N = Half<T>::N;
+  const Sides<T> w = weights_of<T, NEIGHBOURS>(weight, ln);
+  float2 caw[N], sbw[N], saw[N], cbw[N];                   // a' = r (a caw - b sbw), b' = r (a saw + b cbw)
 #pragma unroll
-  for (int j = 0; j < E; ++j) {
-    cw[j] = c[j] * w[j];
-    sw[j] = 0.f;
-    if (ln.e0 + j < a.rot) sw[j] = s[j] * (NEIGHBOURS ? w[j ^ 1] : weight != nullptr ? to_f32<T>(static_cast<const T*>(weight)[e1 + j]) : 1.f);
+  for (int i = 0; i < N; ++i) {
+    caw[i] = mul_pair(c[i], w.a[i]);
+    saw[i] = mul_pair(s[i], w.a[i]);
+    cbw[i] = mul_pair(c[i], w.b[i]);
+    sbw[i] = mul_pair(s[i], mul_pair(w.b[i], twice(-1.f)));
   }
-  const T* x = reinterpret_cast<const T*>(in.p) + b * in.s0 + t * in.s2 + ln.e0;
-  T* y = reinterpret_cast<T*>(out.p) + b * out.s0 + t * out.s2 + ln.e0;
+  const T* x = reinterpret_cast<const T*>(in.p) + b * in.s0 + t * in.s2 + h0 * in.s1;
+  T* y = reinterpret_cast<T*>(out.p) + b * out.s0 + t * out.s2 + h0 * out.s1;
   const float inv_d = 1.f / (float)a.d;
   for (int h = h0; h < h1; h += kAhead) {
-    Entries<T, E> raw[kAhead];
+    Pieces<T> raw[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       raw[u].zero();
-      if (on && h + u < h1) raw[u].load(x + (long long)(h + u) * in.s1);
+      if (on && h + u < h1) raw[u].load(x, ln);
+      x += in.s1;
     }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       if (h + u >= h1) break;
-      float v[E], o[E], ss = 0.f;
-      raw[u].get(v);
-      partner<T, E, NEIGHBOURS>(raw[u], ln.src, o);
+      Sides<T> v = raw[u].template get<NEIGHBOURS>();
+      float2 q = mul_pair(v.a[0], v.a[0]);
+      q = fma_pair(v.b[0], v.b[0], q);
 #pragma unroll
-      for (int j = 0; j < E; ++j) ss = fmaf(v[j], v[j], ss);
-      for (int m = lanes >> 1; m > 0; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
-      const float r = rsqrtf(fmaf(ss, inv_d, a.eps));
-#pragma unroll
-      for (int j = 0; j < E; ++j) v[j] = r * fmaf(o[j], sw[j], v[j] * cw[j]);
-      if (on) {
-        Entries<T, E> st;
-        st.set(v);
-        st.store(y + (long long)(h + u) * out.s1);
+      for (int i = 1; i < N; ++i) {
+        q = fma_pair(v.a[i], v.a[i], q);
+        q = fma_pair(v.b[i], v.b[i], q);
       }
+      const float2 r = twice(rsqrtf(fmaf(row_sum(q.x + q.y, lanes), inv_d, a.eps)));
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float2 xa = mul_pair(v.a[i], r), xb = mul_pair(v.b[i], r);
+        v.a[i] = fma_pair(xb, sbw[i], mul_pair(xa, caw[i]));
+        v.b[i] = fma_pair(xa, saw[i], mul_pair(xb, cbw[i]));
+      }
+      if (on) {
+        Pieces<T> o;
+        o.template set<NEIGHBOURS>(v);
+        o.store(y, ln);
+      }
+      y += out.s1;
     }
   }
 }
@@ -129,88 +207,97 @@ __device__ __forceinline__ long long position(const NormRope& a, long long b, lo
 
 // grid: (groups of tokens, groups of heads_per heads of q and k together)
 template <typename T, bool NEIGHBOURS>
-__global__ void __launch_bounds__(kThreads) norm_rope_kernel(const __grid_constant__ NormRope a, int lanes, int heads_per) {
-  constexpr int E = 16 / sizeof(T);
+__global__ void __launch_bounds__(kThreads, 4) norm_rope_kernel(const __grid_constant__ NormRope a, int lanes, int heads_per) {
   __shared__ unsigned long long turns[64];
   share_turns(a, turns);
   wait_for_kernels_ahead();
-  const int per = kThreads / lanes;
-  const long long tok = (long long)blockIdx.x * per + threadIdx.x / lanes;
-  const bool on = tok < (long long)a.B * a.T;
-  const long long b = on ? tok / a.T : 0, t = on ? tok - b * a.T : 0;
-  const Lane ln = lane_of<E>(a, lanes);
-  float c[E], s[E];
-  turns_of<E, NEIGHBOURS>(a, turns, ln.e0, position(a, b, t), c, s);
+  const unsigned per = kThreads / lanes, tok = blockIdx.x * per + threadIdx.x / lanes;      // (at most 2^31 tokens)
+  const bool on = tok < (unsigned long long)a.B * a.T;
+  const unsigned b = on ? tok / (unsigned)a.T : 0, t = on ? tok - b * (unsigned)a.T : 0;
+  const Lane ln = lane_of<T, NEIGHBOURS>(a, lanes);
+  float2 c[Half<T>::N], s[Half<T>::N];
+  turns_of<T, NEIGHBOURS>(turns, ln, position(a, b, t), c, s);
   const int h0 = blockIdx.y * heads_per, h1 = min(h0 + heads_per, a.Hq + a.Hk);
-  if (h0 < a.Hq) forward_heads<T, E, NEIGHBOURS>(a, a.q, a.q_out, a.q_weight, b, t, h0, min(h1, a.Hq), on, ln, lanes, c, s);
-  if (h1 > a.Hq) forward_heads<T, E, NEIGHBOURS>(a, a.k, a.k_out, a.k_weight, b, t, max(h0, a.Hq) - a.Hq, h1 - a.Hq, on, ln, lanes, c, s);
+  if (h0 < a.Hq) forward_heads<T, NEIGHBOURS>(a, a.q, a.q_out, a.q_weight, b, t, h0, min(h1, a.Hq), on, ln, lanes, c, s);
+  if (h1 > a.Hq) forward_heads<T, NEIGHBOURS>(a, a.k, a.k_out, a.k_weight, b, t, max(h0, a.Hq) - a.Hq, h1 - a.Hq, on, ln, lanes, c, s);
 }
 
-template <typename T, int E, bool NEIGHBOURS>
+template <typename T, bool NEIGHBOURS>
 __device__ __forceinline__ void backward_heads(const NormRope& a, const View& in, const View& grad, const View& out, const void* weight, long long b,
-                                               long long t, int h0, int h1, bool on, const Lane& ln, int lanes, const float (&c)[E],
-                                               const float (&s)[E], float (&dw)[E]) {
-  float w[E];
-  load_weight<T, E>(weight, ln.e0, w);
-  const T* x = reinterpret_cast<const T*>(in.p) + b * in.s0 + t * in.s2 + ln.e0;
-  const T* g = reinterpret_cast<const T*>(grad.p) + b * grad.s0 + t * grad.s2 + ln.e0;
-  T* y = reinterpret_cast<T*>(out.p) + b * out.s0 + t * out.s2 + ln.e0;
+                                               long long t, int h0, int h1, bool on, const Lane& ln, int lanes, const float2 (&c)[Half<T>::N],
+                                               const float2 (&s)[Half<T>::N], Sides<T>& dw) {
+  constexpr int N = Half<T>::N;
+  const Sides<T> w = weights_of<T, NEIGHBOURS>(weight, ln);
+  const T* x = reinterpret_cast<const T*>(in.p) + b * in.s0 + t * in.s2 + h0 * in.s1;
+  const T* g = reinterpret_cast<const T*>(grad.p) + b * grad.s0 + t * grad.s2 + h0 * grad.s1;
+  T* y = reinterpret_cast<T*>(out.p) + b * out.s0 + t * out.s2 + h0 * out.s1;
   const float inv_d = 1.f / (float)a.d;
-  constexpr int AHEAD = kAhead / 2;
-  for (int h = h0; h < h1; h += AHEAD) {
-    Entries<T, E> raw[AHEAD], graw[AHEAD];
+  for (int h = h0; h < h1; h += kBwdAhead) {
+    Pieces<T> raw[kBwdAhead], graw[kBwdAhead];
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
+    for (int u = 0; u < kBwdAhead; ++u) {
       raw[u].zero();
       graw[u].zero();
       if (on && h + u < h1) {
-        raw[u].load(x + (long long)(h + u) * in.s1);
-        graw[u].load(g + (long long)(h + u) * grad.s1);
+        raw[u].load(x, ln);
+        graw[u].load(g, ln);
       }
+      x += in.s1;
+      g += grad.s1;
     }
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
+    for (int u = 0; u < kBwdAhead; ++u) {
       if (h + u >= h1) break;
-      float v[E], z[E], o[E], ss = 0.f, dot = 0.f;
-      raw[u].get(v);
-      graw[u].get(z);
-      partner<T, E, NEIGHBOURS>(graw[u], ln.src, o);
+      Sides<T> v = raw[u].template get<NEIGHBOURS>(), z = graw[u].template get<NEIGHBOURS>();
+      float2 q = twice(0.f), dot = twice(0.f);
 #pragma unroll
-      for (int j = 0; j < E; ++j) {
-        z[j] = fmaf(-s[j], o[j], z[j] * c[j]);              // the turn back
-        ss = fmaf(v[j], v[j], ss);
-        dot = fmaf(z[j] * w[j], v[j], dot);
+      for (int i = 0; i < N; ++i) {                        // the turn back
+        const float2 za = fma_pair(z.b[i], s[i], mul_pair(z.a[i], c[i]));
+        z.b[i] = fma_pair(z.b[i], c[i], mul_pair(mul_pair(z.a[i], twice(-1.f)), s[i]));
+        z.a[i] = za;
+        q = fma_pair(v.a[i], v.a[i], q);
+        q = fma_pair(v.b[i], v.b[i], q);
+        dot = fma_pair(mul_pair(z.a[i], w.a[i]), v.a[i], dot);
+        dot = fma_pair(mul_pair(z.b[i], w.b[i]), v.b[i], dot);
       }
-      for (int m = lanes >> 1; m > 0; m >>= 1) {
-        ss += __shfl_xor_sync(0xffffffffu, ss, m);
-        dot += __shfl_xor_sync(0xffffffffu, dot, m);
-      }
-      const float r = on ? rsqrtf(fmaf(ss, inv_d, a.eps)) : 0.f;
-      const float m = dot * r * r * inv_d;
+      // (every lane takes part in the sums, also one without a token)
+      const float square = row_sum(q.x + q.y, lanes), product = row_sum(dot.x + dot.y, lanes);
+      const float rr = on ? rsqrtf(fmaf(square, inv_d, a.eps)) : 0.f;
+      const float2 r = twice(rr), m = twice(-product * rr * rr * inv_d);
 #pragma unroll
-      for (int j = 0; j < E; ++j) {
-        dw[j] = fmaf(z[j], v[j] * r, dw[j]);
-        v[j] = r * fmaf(-m, v[j], z[j] * w[j]);
+      for (int i = 0; i < N; ++i) {
+        const float2 xa = mul_pair(v.a[i], r), xb = mul_pair(v.b[i], r);
+        dw.a[i] = fma_pair(z.a[i], xa, dw.a[i]);
+        dw.b[i] = fma_pair(z.b[i], xb, dw.b[i]);
+        v.a[i] = fma_pair(xa, m, mul_pair(mul_pair(z.a[i], w.a[i]), r));
+        v.b[i] = fma_pair(xb, m, mul_pair(mul_pair(z.b[i], w.b[i]), r));
       }
       if (on) {
-        Entries<T, E> st;
-        st.set(v);
-        st.store(y + (long long)(h + u) * out.s1);
+        Pieces<T> o;
+        o.template set<NEIGHBOURS>(v);
+        o.store(y, ln);
       }
+      y += out.s1;
     }
   }
 }
 
 // Sums of the weights' gradients over the lanes and warps of a block: part[d].  Fixed order.
-template <int E>
-__device__ __forceinline__ void block_sum(float (&dw)[E], int lanes, int e0, int d, float* red, float* part) {
+template <typename T, bool NEIGHBOURS>
+__device__ __forceinline__ void block_sum(const Sides<T>& dw, int lanes, const Lane& ln, int d, float* red, float* part) {
+  constexpr int E = Half<T>::E, N = Half<T>::N;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll
-  for (int j = 0; j < E; ++j)
-    for (int m = lanes; m < 32; m <<= 1) dw[j] += __shfl_xor_sync(0xffffffffu, dw[j], m);
-  if (lane < lanes)
+  for (int i = 0; i < N; ++i) {
+    float v[4] = {dw.a[i].x, dw.a[i].y, dw.b[i].x, dw.b[i].y};
 #pragma unroll
-    for (int j = 0; j < E; ++j) red[warp * 128 + e0 + j] = dw[j];
+    for (int k = 0; k < 4; ++k) {
+      for (int m = lanes; m < 32; m <<= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], m);
+      // entry of side k / 2, number 2 i + k % 2 of this lane's
+      const int j = 2 * i + (k & 1), e = NEIGHBOURS ? 2 * j + (k >> 1) : (k >> 1) * E + j;
+      if (lane < lanes) red[warp * 128 + (e < E ? ln.e0 + e : ln.e1 + e - E)] = v[k];
+    }
+  }
   __syncthreads();
   for (int e = threadIdx.x; e < d; e += kThreads) {
     float sum = 0.f;
@@ -223,49 +310,55 @@ __device__ __forceinline__ void block_sum(float (&dw)[E], int lanes, int e0, int
 
 // part: [blocks][2][d] (queries, keys), or null
 template <typename T, bool NEIGHBOURS>
-__global__ void __launch_bounds__(kThreads) norm_rope_bwd_kernel(const __grid_constant__ NormRope a, int lanes, int heads_per, long long tok_groups,
-                                                                 float* __restrict__ part) {
-  constexpr int E = 16 / sizeof(T);
+__global__ void __launch_bounds__(kThreads, 3) norm_rope_bwd_kernel(const __grid_constant__ NormRope a, int lanes, int heads_per, unsigned tok_groups,
+                                                                    float* __restrict__ part) {
   __shared__ unsigned long long turns[64];
   __shared__ float red[kThreads / 32 * 128];
   share_turns(a, turns);
   wait_for_kernels_ahead();
-  const int per = kThreads / lanes;
-  const Lane ln = lane_of<E>(a, lanes);
+  const unsigned per = kThreads / lanes;
+  const Lane ln = lane_of<T, NEIGHBOURS>(a, lanes);
   const int h0 = blockIdx.y * heads_per, h1 = min(h0 + heads_per, a.Hq + a.Hk);
-  float dqw[E], dkw[E];
+  Sides<T> dqw, dkw;
 #pragma unroll
-  for (int j = 0; j < E; ++j) dqw[j] = dkw[j] = 0.f;
-  for (long long grp = blockIdx.x; grp < tok_groups; grp += gridDim.x) {
-    const long long tok = grp * per + threadIdx.x / lanes;
-    const bool on = tok < (long long)a.B * a.T;
-    const long long b = on ? tok / a.T : 0, t = on ? tok - b * a.T : 0;
-    float c[E], s[E];
-    turns_of<E, NEIGHBOURS>(a, turns, ln.e0, position(a, b, t), c, s);
-    if (h0 < a.Hq) backward_heads<T, E, NEIGHBOURS>(a, a.q, a.q_out, a.dq, a.q_weight, b, t, h0, min(h1, a.Hq), on, ln, lanes, c, s, dqw);
+  for (int i = 0; i < Half<T>::N; ++i) dqw.a[i] = dqw.b[i] = dkw.a[i] = dkw.b[i] = twice(0.f);
+  for (unsigned grp = blockIdx.x; grp < tok_groups; grp += gridDim.x) {
+    const unsigned long long tok = (unsigned long long)grp * per + threadIdx.x / lanes;
+    const bool on = tok < (unsigned long long)a.B * a.T;
+    const unsigned b = on ? (unsigned)tok / (unsigned)a.T : 0, t = on ? (unsigned)tok - b * (unsigned)a.T : 0;
+    float2 c[Half<T>::N], s[Half<T>::N];
+    turns_of<T, NEIGHBOURS>(turns, ln, position(a, b, t), c, s);
+    if (h0 < a.Hq) backward_heads<T, NEIGHBOURS>(a, a.q, a.q_out, a.dq, a.q_weight, b, t, h0, min(h1, a.Hq), on, ln, lanes, c, s, dqw);
     if (h1 > a.Hq)
-      backward_heads<T, E, NEIGHBOURS>(a, a.k, a.k_out, a.dk, a.k_weight, b, t, max(h0, a.Hq) - a.Hq, h1 - a.Hq, on, ln, lanes, c, s, dkw);
+      backward_heads<T, NEIGHBOURS>(a, a.k, a.k_out, a.dk, a.k_weight, b, t, max(h0, a.Hq) - a.Hq, h1 - a.Hq, on, ln, lanes, c, s, dkw);
   }
   if (part == nullptr) return;
   float* mine = part + ((size_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 * a.d;
-  block_sum<E>(dqw, lanes, ln.e0, a.d, red, mine);
-  block_sum<E>(dkw, lanes, ln.e0, a.d, red, mine + a.d);
+  block_sum<T, NEIGHBOURS>(dqw, lanes, ln, a.d, red, mine);
+  block_sum<T, NEIGHBOURS>(dkw, lanes, ln, a.d, red, mine + a.d);
 }
 
-// One block per tensor: the blocks' sums, 1024 / d runs of them side by side, then the runs in order.
-__global__ void __launch_bounds__(1024) norm_rope_sum_kernel(const float* __restrict__ part, int blocks, int d, float* __restrict__ dq_weight,
-                                                             float* __restrict__ dk_weight) {
-  __shared__ float red[1024];
+// Eight entries of a tensor's weights per block: the blocks' sums, 32 runs of them side by side, then the runs in order.
+__global__ void __launch_bounds__(256) norm_rope_sum_kernel(const float* __restrict__ part, int blocks, int d, float* __restrict__ dq_weight,
+                                                            float* __restrict__ dk_weight) {
+  __shared__ float red[32][9];
   wait_for_kernels_ahead();
   float* to = blockIdx.x == 0 ? dq_weight : dk_weight;
   if (to == nullptr) return;
-  const int e = threadIdx.x % d, y = threadIdx.x / d, ny = 1024 / d;
+  const int i = threadIdx.x & 7, y = threadIdx.x >> 3, e = blockIdx.y * 8 + i;
   float sum = 0.f;
-  for (int b = y; b < blocks; b += ny) sum += part[((size_t)b * 2 + blockIdx.x) * d + e];
-  red[threadIdx.x] = sum;
+  for (int b = y; b < blocks; b += 8 * 32) {
+    float v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = b + u * 32 < blocks ? part[((size_t)(b + u * 32) * 2 + blockIdx.x) * d + e] : 0.f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) sum += v[u];
+  }
+  red[y][i] = sum;
   __syncthreads();
   if (y != 0) return;
-  for (int i = 1; i < ny; ++i) sum += red[i * d + e];
+#pragma unroll
+  for (int k = 1; k < 32; ++k) sum += red[k][i];
   to[e] = sum;
 }
 
@@ -274,31 +367,30 @@ struct RopeGrid {
   long long tok_groups;
   dim3 grid;
 };
-// All heads of a token in one block, or fewer (down to one step of the loop) while there are fewer blocks than fill the GPU.
-RopeGrid rope_grid(int B, int T, int H, int d, int elem, int step, long long max_x) {
+// Heads of a token in two blocks, or in more (down to `step` heads) while there are fewer blocks than fill the GPU. 
+RopeGrid rope_grid(int B, int T, int H, int d, int elem, int step, bool backward) {
   RopeGrid g;
   g.lanes = d * elem / 16;
   const int per = kThreads / g.lanes;
   g.tok_groups = ((long long)B * T + per - 1) / per;
-  long long x = g.tok_groups < max_x ? g.tok_groups : max_x;
-  g.heads_per = H;
-  while (g.heads_per > step && x * ((H + g.heads_per - 1) / g.heads_per) < 4 * kPlanSMs) g.heads_per = (g.heads_per + 1) / 2;
-  g.grid = dim3((unsigned)x, (unsigned)((H + g.heads_per - 1) / g.heads_per));
+  g.heads_per = (H + 1) / 2 > step ? (H + 1) / 2 : step;
+  while (g.heads_per > step && g.tok_groups * ((H + g.heads_per - 1) / g.heads_per) < kBlocks) g.heads_per = (g.heads_per + 1) / 2;
+  const long long y = (H + g.heads_per - 1) / g.heads_per, most = backward ? (kBlocks + y - 1) / y : g.tok_groups;
+  g.grid = dim3((unsigned)(g.tok_groups < most ? g.tok_groups : most), (unsigned)y);
   return g;
 }
-constexpr int kBwdStep = kAhead / 2;
 
 template <typename T> void forward(const NormRope& a, LaunchCtx& ctx) {
-  const RopeGrid g = rope_grid(a.B, a.T, a.Hq + a.Hk, a.d, sizeof(T), 1, (1LL << 31) - 1);
+  const RopeGrid g = rope_grid(a.B, a.T, a.Hq + a.Hk, a.d, sizeof(T), 1, false);
   launch_after(ctx, a.interleaved ? norm_rope_kernel<T, true> : norm_rope_kernel<T, false>, g.grid, dim3(kThreads), 0, a, g.lanes, g.heads_per);
 }
 
 template <typename T> void backward(const NormRope& a, float* ws, LaunchCtx& ctx) {
-  const RopeGrid g = rope_grid(a.B, a.T, a.Hq + a.Hk, a.d, sizeof(T), kBwdStep, kMaxBwdBlocks);
+  const RopeGrid g = rope_grid(a.B, a.T, a.Hq + a.Hk, a.d, sizeof(T), kBwdAhead, true);
   const bool sums = a.dq_weight != nullptr || a.dk_weight != nullptr;
   launch_after(ctx, a.interleaved ? norm_rope_bwd_kernel<T, true> : norm_rope_bwd_kernel<T, false>, g.grid, dim3(kThreads), 0, a, g.lanes, g.heads_per,
-               g.tok_groups, sums ? ws : nullptr);
-  if (sums) launch_after(ctx, norm_rope_sum_kernel, dim3(2), dim3(1024), 0, ws, (int)(g.grid.x * g.grid.y), a.d, a.dq_weight, a.dk_weight);
+               (unsigned)g.tok_groups, sums ? ws : nullptr);
+  if (sums) launch_after(ctx, norm_rope_sum_kernel, dim3(2, a.d / 8), dim3(256), 0, ws, (int)(g.grid.x * g.grid.y), a.d, a.dq_weight, a.dk_weight);
 }
 
 }  // namespace
@@ -312,7 +404,7 @@ void norm_rope_fwd(const NormRope& a, LaunchCtx& ctx) {
 size_t norm_rope_bwd_workspace_elems(int B, int T, int H, int d) {
   size_t blocks = 0;
   for (int elem = 2; elem <= 4; elem += 2) {
-    const RopeGrid g = rope_grid(B, T, H, d, elem, kBwdStep, kMaxBwdBlocks);
+    const RopeGrid g = rope_grid(B, T, H, d, elem, kBwdAhead, true);
     if ((size_t)g.grid.x * g.grid.y > blocks) blocks = (size_t)g.grid.x * g.grid.y;
   }
   return blocks * 2 * d;
