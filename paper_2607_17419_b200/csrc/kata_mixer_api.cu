@@ -191,7 +191,7 @@ int ssm(const kata_ssm_args* a, const kata_opts* opts, bool step) {
   for (const void* p : {(const void*)a->A, (const void*)a->D, (const void*)a->dt_bias, (const void*)a->lengths})
     if ((reinterpret_cast<uintptr_t>(p) & 3u) != 0) return KATA_ERR_ALIGNMENT;
   if ((reinterpret_cast<uintptr_t>(a->s_init) & 15u) != 0 || (reinterpret_cast<uintptr_t>(a->s_final) & 15u) != 0) return KATA_ERR_ALIGNMENT;
-  const SsmPlan plan = step ? SsmPlan{1, 1} : ssm_plan(a->B * a->H, T, tensor);
+  const SsmPlan plan = step ? SsmPlan{1, 1} : ssm_plan(a->B * a->H, T, tensor, r.s_final != nullptr);
   if (tensor && T > 1 && (r.q.s2 == 0 || r.k.s2 == 0 || r.v.s2 == 0)) {      // (one row for all tokens has no tensor map)
     if (o.impl == KATA_IMPL_TENSOR) return KATA_ERR_UNSUPPORTED_SHAPE;
     tensor = false;
@@ -216,8 +216,10 @@ size_t mixer_workspace_bytes(int fn, int B, int H, int T, int d_k, int d_v, cons
   if (fn == KATA_FN_BWD_SHORT_CONV)
     return d_k >= 2 && d_k <= 4 && H <= (1 << 24) && (double)B * T * H <= 1e11 ? align_up(short_conv_bwd_workspace_elems(B, T, H, d_k) * sizeof(float)) : 0;
   if (ssm_shape(B, H, T, d_k, d_v) != KATA_OK) return 0;
+  // (what a call with or without a final state takes)
   const bool tensor = ssm_tensor(o, d_k, d_v);
-  return align_up(ssm_workspace_bytes(B * H, d_k, d_v, ssm_slots(ssm_plan(B * H, T, tensor), tensor, true)));      // (with a final state)
+  const int with = ssm_slots(ssm_plan(B * H, T, tensor, true), tensor, true), without = ssm_slots(ssm_plan(B * H, T, tensor, false), tensor, false);
+  return align_up(ssm_workspace_bytes(B * H, d_k, d_v, with > without ? with : without));
 }
 
 }  // namespace kata

@@ -202,17 +202,19 @@ template <typename T> void by_rows(const Ssm& a, const SsmPlan& plan, float* ws,
 
 }  // namespace
 
-// Segments of whole 128-token tiles.  The second pass takes whole waves of CTAs (one per SM on the tensor cores, four of the token by
-// token kernel), the first one nearly as long again and two launches more; the number of segments with the smallest sum.
-SsmPlan ssm_plan(int BH, int T, bool tensor) {
+// Segments of whole 128-token tiles.  The passes take whole waves of CTAs (one per SM on the tensor cores, four of the token by token
+// kernel); several segments, and a final state on the tensor cores, take the pass of the states too.  The number of segments with the
+// smallest sum.  Measured, us a tile, outputs and states: tensor cores 1.85 and 0.75 (n = 64), token by token 8 and 6.5.
+SsmPlan ssm_plan(int BH, int T, bool tensor, bool final_state) {
   const int tiles = (T + 127) / 128, resident = kPlanSMs * (tensor ? 1 : 4);
-  const double tile_us = tensor ? 0.8 : 8.0;
+  const double out_us = tensor ? 1.85 : 8.0, state_us = tensor ? 0.75 : 6.5;
   SsmPlan best{1, tiles * 128};
-  double best_us = ceil((double)BH / resident) * tiles * tile_us;
-  for (int want = 2; want <= tiles && (long long)BH * (want - 1) < 2LL * resident; ++want) {
+  double best_us = 0.0;
+  for (int want = 1; want <= tiles && (want == 1 || (long long)BH * (want - 1) < 2LL * resident); ++want) {
     const int per = (tiles + want - 1) / want, n = (tiles + per - 1) / per;
-    const double us = ceil((double)BH * n / resident) * per * tile_us * 1.8 + 8.0 + 0.1 * n;
-    if (us < best_us) {
+    const bool states = n > 1 || (tensor && final_state);
+    const double us = ceil((double)BH * n / resident) * per * (out_us + (states ? state_us : 0.0)) + (states ? 8.0 + 0.1 * n : 0.0);
+    if (want == 1 || us < best_us) {
       best_us = us;
       best = SsmPlan{n, per * 128};
     }

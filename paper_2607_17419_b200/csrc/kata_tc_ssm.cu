@@ -11,11 +11,12 @@
 // The weights of a 32 x 32 block are a row factor times a column factor, taken at the start of the rows' block: below the diagonal
 // both are at most s_i; on the diagonal they are taken at half of the block's decay, and only blocks that decay by more than 2^-240 in
 // their 32 tokens take an exponential per entry instead.  So a tile takes a few exponentials per token and two products per score.
-// tc_ssm_state_kernel: the segments' own states (several segments, or a final state wanted), exact to fp32: the scaled V goes in
-// as three bf16 terms (24 bits), the small ones first, and every tile's product is added in registers.
+// tc_ssm_state_kernel: the segments' own states (several segments, or a final state wanted).  For a final state they are exact to
+// fp32: the scaled V goes in as three bf16 terms (24 bits), the small ones first; every tile's product is added in registers.
 //
 // Warps.  Out (768 threads): 0 decays; 1 issues Q K^T and Q S, 2 the tile's state and the product with V; 3 TMA loads;
-// 4-7 state; 8-15 weights and 16-23 scaled V and epilogue, two warps per TMEM lane quadrant.  State (512): 8-15 scaled V.  A warp reaches the next wait of its job long before the
+// 4-7 state; 8-15 weights and 16-23 scaled V and epilogue, two warps per TMEM lane quadrant.  State (512): 0 loads, 1 issues, 2, 3 decays, 4-7
+// state, 8-15 scaled V.  A warp reaches the next wait of its job long before the
 // others are done with theirs, so a tile takes the longest job and not their sum.  The jobs' loops are written once each and kept short: sixteen warps in unlike code of some thousand instructions each waited for instructions most of
 // the time (8 x 16 heads x 4096 tokens 135 us).  All waits are bounded; a warp that has TMEM to read goes on only where all its
 // lanes saw the barrier.
@@ -53,12 +54,12 @@ struct Decays {
   float pad[2];
 };
 
-template <int N, bool STATE> struct Shape {
+template <int N, int STATE> struct Shape {         // STATE: terms of the scaled V in the state kernel; 0: the out kernel
   static constexpr int HALVES = N / 64;                                        // 64-column halves of a q or k tile
   static constexpr uint32_t K_OFF = STATE ? 0 : HALVES * HALF, V_OFF = K_OFF + HALVES * HALF;
   static constexpr uint32_t STAGE = V_OFF + HALF;
   static constexpr int NST = STATE ? (N == 64 ? 3 : 2) : (N == 64 ? 3 : 2);
-  static constexpr int TERMS = STATE ? 3 : 1;
+  static constexpr int TERMS = STATE ? STATE : 1;
   static constexpr int XB = !STATE && N == 128 ? 1 : 2;                        // buffers of scaled V
   static constexpr uint32_t OFF_X = NST * STAGE;
   static constexpr uint32_t OFF_S = OFF_X + XB * TERMS * HALF;                 // [N][64] bf16
@@ -67,9 +68,9 @@ template <int N, bool STATE> struct Shape {
   static constexpr uint32_t OFF_BAR = OFF_DEC + NSLOT * sizeof(Decays);
   static constexpr uint32_t SMEM = OFF_BAR + 512 + 1024;
 };
-static_assert(Shape<128, false>::SMEM <= 232448 && Shape<64, false>::SMEM <= 232448, "shared memory");
-static_assert(Shape<128, true>::SMEM <= 232448 && Shape<64, true>::SMEM <= 232448, "shared memory");
-static_assert(Shape<64, false>::SMEM > 116 * 1024 && Shape<64, true>::SMEM > 116 * 1024, "one CTA per SM is assumed (it takes all of TMEM)");
+static_assert(Shape<128, 0>::SMEM <= 232448 && Shape<64, 0>::SMEM <= 232448, "shared memory");
+static_assert(Shape<128, 3>::SMEM <= 232448 && Shape<64, 3>::SMEM <= 232448, "shared memory");
+static_assert(Shape<64, 0>::SMEM > 116 * 1024 && Shape<64, 1>::SMEM > 116 * 1024, "one CTA per SM is assumed (it takes all of TMEM)");
 
 constexpr uint32_t COL_P = 0;                    // 2 x 128: scores; the bf16 weights overwrite columns [0,32) and [64,96) of a buffer
 constexpr uint32_t COL_Y = 256, COL_R = 320;     // product with V, Q S
@@ -167,10 +168,10 @@ __device__ __forceinline__ Where where(const Args& a) {
   return w;
 }
 
-// Decays of the tiles, one warp: a lane has four neighbouring tokens, eight lanes a block; the next tile's steps are on their way.
-// ALL: the factors of the weights too.  Returns the logarithm (base 2) of the decay over all tiles.
-template <bool ALL>
-__device__ __forceinline__ double decay_warp(const Args& a, const Where& w, Decays* slots, uint64_t* bars, volatile int* abort_flag, bool& ok) {
+// Decays of every STRIDE-th tile from `first` on, one warp: a lane has four neighbouring tokens, eight lanes a block; the next tile's
+// steps are on their way.  ALL: the factors of the weights too.  Returns the logarithm (base 2) of the decay over these tiles.
+template <bool ALL, int STRIDE>
+__device__ __forceinline__ double decay_warp(int first, const Args& a, const Where& w, Decays* slots, uint64_t* bars, volatile int* abort_flag, bool& ok) {
   const int lane = threadIdx.x & 31;
   const __nv_bfloat16* dt = static_cast<const __nv_bfloat16*>(a.dt) + w.b * a.dt0 + w.h * a.dt1;
   const float rate = (float)((double)a.A[w.h] * 1.4426950408889634074);
@@ -184,9 +185,9 @@ __device__ __forceinline__ double decay_warp(const Args& a, const Where& w, Deca
       next[i] = dt[(long long)min(t, w.live - 1) * a.dt2];
     }
   };
-  if (w.tiles > 0) fetch(0);
+  if (first < w.tiles) fetch(first);
 #pragma unroll 1
-  for (int j = 0; j < w.tiles; ++j) {
+  for (int j = first; j < w.tiles; j += STRIDE) {
     float s[4], c[4], sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -196,7 +197,7 @@ __device__ __forceinline__ double decay_warp(const Args& a, const Where& w, Deca
       sum = fmaf(s[i], rate, sum);
       c[i] = sum;
     }
-    if (j + 1 < w.tiles) fetch(j + 1);
+    if (j + STRIDE < w.tiles) fetch(j + STRIDE);
     float upto = sum;                            // from the start of the block
 #pragma unroll
     for (int off = 1; off < 8; off <<= 1) {
@@ -292,7 +293,7 @@ template <int N>
 __global__ void __launch_bounds__(kOutThreads, 1)
 tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                   const __grid_constant__ CUtensorMap tmO, const __grid_constant__ Args a) {
-  typedef Shape<N, false> Sh;
+  typedef Shape<N, 0> Sh;
   constexpr int NST = Sh::NST, XB = Sh::XB, KS = N / 16;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* base = aligned_base(smem_raw);
@@ -339,7 +340,7 @@ tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 
   if (warp == 0) {
     // =========================== decays ===========================
-    decay_warp<true>(a, w, decays, bars, abort_flag, ok);
+    decay_warp<true, 1>(0, a, w, decays, bars, abort_flag, ok);
   } else if (warp == 1) {
     // =========================== scores Q K^T, one tile ahead, and Q S ===========================
     const uint32_t id_qk = instr_desc(kFmtBF16, kFmtBF16, 0, 0, 128, 128), id_r = instr_desc(kFmtBF16, kFmtBF16, 0, 1, 128, DV);
@@ -665,10 +666,10 @@ tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     *reinterpret_cast<uint4*>(a.out + w.b * a.o0 + w.h * a.o1 + (first + (i >> 3)) * a.o2 + (i & 7) * 8) = make_uint4(0u, 0u, 0u, 0u);
 }
 
-template <int N>
+template <int N, int TERMS>
 __global__ void __launch_bounds__(kStateThreads, 1)
 tc_ssm_state_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ Args a) {
-  typedef Shape<N, true> Sh;
+  typedef Shape<N, TERMS> Sh;
   constexpr int NST = Sh::NST;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* base = aligned_base(smem_raw);
@@ -676,9 +677,10 @@ tc_ssm_state_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   Decays* decays = reinterpret_cast<Decays*>(base + Sh::OFF_DEC);
   auto ktile = [&](int s) { return base + s * Sh::STAGE; };
   auto vtile = [&](int s) { return base + s * Sh::STAGE + Sh::V_OFF; };
-  auto xtile = [&](int j, int term) { return base + Sh::OFF_X + ((j & 1) * 3 + term) * HALF; };
+  auto xtile = [&](int j, int term) { return base + Sh::OFF_X + ((j & 1) * TERMS + term) * HALF; };
   __shared__ uint32_t tmem_base_s;
   __shared__ int abort_s;
+  __shared__ double all_s[2];                    // logarithms of the decay over the two warps' tiles
   volatile int* abort_flag = &abort_s;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   bool ok = true;
@@ -735,11 +737,11 @@ tc_ssm_state_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
         const uint32_t ka = smem_u32(ktile(s));
         tc_fence_after();
 #pragma unroll
-        for (int m = 2; m >= 0; --m) {           // (the small terms first)
+        for (int m = TERMS - 1; m >= 0; --m) {           // (the small terms first)
           const uint32_t xa = smem_u32(xtile(j, m));
 #pragma unroll
           for (int ks = 0; ks < CT / 16; ++ks)
-            mma_f16_ss(tb + COL_SL + b * DV, at(dn, ka + ks * 2048), at(dn, xa + ks * 2048), id_s, m < 2 || ks > 0);
+            mma_f16_ss(tb + COL_SL + b * DV, at(dn, ka + ks * 2048), at(dn, xa + ks * 2048), id_s, m + 1 < TERMS || ks > 0);
         }
         mma_commit(bars + BAR_SL_FULL + b);
         mma_commit(bars + BAR_X_EMPTY + b);
@@ -747,10 +749,10 @@ tc_ssm_state_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
       }
       __syncwarp();
     }
-  } else if (warp == 3) {
-    // =========================== decays ===========================
-    const double all = decay_warp<false>(a, w, decays, bars, abort_flag, ok);
-    if (lane == 0) a.decay[(size_t)w.bh * a.slots + w.seg] = ex2((float)all);
+  } else if (warp < W_STATE0) {
+    // =========================== decays, every other tile ===========================
+    const double part = decay_warp<false, 2>(warp - 2, a, w, decays, bars, abort_flag, ok);
+    if (lane == 0) all_s[warp - 2] = part;
   } else if (warp >= W_STATE0 && warp < W_WEIGHT0) {
     // =========================== state ===========================
     const int q4 = warp & 3, row = state_row<N>(q4, lane);
@@ -798,15 +800,15 @@ tc_ssm_state_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
 #pragma unroll
       for (int c = 4 * ch; c < 4 * ch + 4; ++c) {
         const uint32_t off = sw128_offset(tok, c);
-        uint4 v = *reinterpret_cast<const uint4*>(vtile(s) + off), x[3];
+        uint4 v = *reinterpret_cast<const uint4*>(vtile(s) + off), x[TERMS];
         if (dead) {                              // (K times zero has to be zero, whatever lies there)
           v = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
           for (int i = 0; i < Sh::HALVES; ++i) *reinterpret_cast<uint4*>(ktile(s) + i * HALF + off) = v;
         }
-        scaled_terms<3>(v, left, x);
+        scaled_terms<TERMS>(v, left, x);
 #pragma unroll
-        for (int m = 0; m < 3; ++m) *reinterpret_cast<uint4*>(xtile(j, m) + off) = x[m];
+        for (int m = 0; m < TERMS; ++m) *reinterpret_cast<uint4*>(xtile(j, m) + off) = x[m];
       }
       fence_async_smem();
       mbar_arrive(bars + BAR_X_FULL + b);
@@ -824,6 +826,7 @@ tc_ssm_state_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   }
   __syncthreads();
   if (warp == 0) tmem_dealloc(tb, TMEM_COLS);
+  if (tid == 0) a.decay[(size_t)w.bh * a.slots + w.seg] = ex2((float)(all_s[0] + all_s[1]));
 }
 
 // [B][heads][T][width] bf16 view, box = cols x rows x 1 x 1; axes that are broadcast (stride 0) have one entry and a coordinate of 0.
@@ -846,7 +849,8 @@ template <int N> void launch(const Ssm& a, const SsmPlan& plan, float* ws, int* 
   int on[2];
   if (!make_view_map(&tmQ, a.q, a.B, a.G, a.T, N, 64, CT, &r.qg, &r.qb) || !make_view_map(&tmK, a.k, a.B, a.G, a.T, N, 64, CT, &r.kg, &r.kb) ||
       !make_view_map(&tmV, a.v, a.B, a.H, a.T, DV, 64, CT, &r.vh, &r.vb) || !make_view_map(&tmO, a.out, a.B, a.H, a.T, DV, 32, 32, &on[0], &on[1]) ||
-      !allow_smem<tc_ssm_out_kernel<N>>((int)Shape<N, false>::SMEM) || !allow_smem<tc_ssm_state_kernel<N>>((int)Shape<N, true>::SMEM)) {
+      !allow_smem<tc_ssm_out_kernel<N>>((int)Shape<N, 0>::SMEM) || !allow_smem<tc_ssm_state_kernel<N, 1>>((int)Shape<N, 1>::SMEM) ||
+      !allow_smem<tc_ssm_state_kernel<N, 3>>((int)Shape<N, 3>::SMEM)) {
     ctx.status = KATA_ERR_CUDA;
     return;
   }
@@ -865,11 +869,13 @@ template <int N> void launch(const Ssm& a, const SsmPlan& plan, float* ws, int* 
   if (states) {
     r.local = ws;
     r.decay = ws + (size_t)a.B * a.H * r.slots * (N * DV);
-    launch_after(ctx, tc_ssm_state_kernel<N>, grid, dim3(kStateThreads), Shape<N, true>::SMEM, tmK, tmV, r);
+    // a final state: to the precision of fp32; states that only outputs read, through their bf16 copy: one term
+    if (a.s_final != nullptr) launch_after(ctx, tc_ssm_state_kernel<N, 3>, grid, dim3(kStateThreads), Shape<N, 3>::SMEM, tmK, tmV, r);
+    else launch_after(ctx, tc_ssm_state_kernel<N, 1>, grid, dim3(kStateThreads), Shape<N, 1>::SMEM, tmK, tmV, r);
     ssm_prefix(a, plan, r.slots, ws, ctx);
     r.init = ws;
   }
-  launch_after(ctx, tc_ssm_out_kernel<N>, grid, dim3(kOutThreads), Shape<N, false>::SMEM, tmQ, tmK, tmV, tmO, r);
+  launch_after(ctx, tc_ssm_out_kernel<N>, grid, dim3(kOutThreads), Shape<N, 0>::SMEM, tmQ, tmK, tmV, tmO, r);
 }
 
 }  // namespace
