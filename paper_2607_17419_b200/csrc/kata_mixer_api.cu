@@ -153,7 +153,13 @@ int ssm_shape(int B, int H, int T, int n, int d) {
   return KATA_OK;
 }
 
-bool ssm_tensor(const CallOpts& o, int n, int d) { return o.impl != KATA_IMPL_SIMT && tc_ssm_supported(o.dtype, n, d); }
+// A tile of the tensor cores is 128 tokens, and a final state takes a pass and a launch more: short sequences go token by token.
+// Measured, us, tensor cores / token by token (n = 64), with a final state: 2048 heads, T = 16: 222 / 29, 64: 225 / 93; 64 heads, T = 64:
+// 14.4 / 11.9; 16 heads, T = 100: 12.3 / 18.8; without: 2048 heads, T = 16: 81 / 27, 32: 81 / 48, 64: 81 / 91; 64 heads, T = 32: 6.2 / 6.8.
+bool ssm_tensor(const CallOpts& o, int n, int d, int T, bool final_state) {
+  if (o.impl == KATA_IMPL_SIMT || !tc_ssm_supported(o.dtype, n, d)) return false;
+  return o.impl == KATA_IMPL_TENSOR || T > (final_state ? 64 : 32);
+}
 
 // Slots of states in the scratch (see SsmPlan).
 int ssm_slots(const SsmPlan& plan, bool tensor, bool final_state) {
@@ -168,7 +174,7 @@ int ssm(const kata_ssm_args* a, const kata_opts* opts, bool step) {
   const int T = step ? 1 : a->T;
   KATA_TRY(ssm_shape(a->B, a->H, T, a->n, a->d_v));
   if (a->G < 1 || a->H % a->G != 0) return KATA_ERR_INVALID_ARG;
-  bool tensor = !step && ssm_tensor(o, a->n, a->d_v);
+  bool tensor = !step && ssm_tensor(o, a->n, a->d_v, T, a->s_final != nullptr);
   if (o.impl == KATA_IMPL_TENSOR && !tensor) return KATA_ERR_UNSUPPORTED_SHAPE;
   if (a->A == nullptr || a->dt == nullptr) return KATA_ERR_INVALID_ARG;
   if (step && (a->s_init == nullptr || a->s_final != a->s_init || a->lengths != nullptr)) return KATA_ERR_INVALID_ARG;
@@ -217,9 +223,13 @@ size_t mixer_workspace_bytes(int fn, int B, int H, int T, int d_k, int d_v, cons
     return d_k >= 2 && d_k <= 4 && H <= (1 << 24) && (double)B * T * H <= 1e11 ? align_up(short_conv_bwd_workspace_elems(B, T, H, d_k) * sizeof(float)) : 0;
   if (ssm_shape(B, H, T, d_k, d_v) != KATA_OK) return 0;
   // (what a call with or without a final state takes)
-  const bool tensor = ssm_tensor(o, d_k, d_v);
-  const int with = ssm_slots(ssm_plan(B * H, T, tensor, true), tensor, true), without = ssm_slots(ssm_plan(B * H, T, tensor, false), tensor, false);
-  return align_up(ssm_workspace_bytes(B * H, d_k, d_v, with > without ? with : without));
+  int slots = 0;
+  for (const bool last : {false, true}) {
+    const bool tensor = ssm_tensor(o, d_k, d_v, T, last);
+    const int n = ssm_slots(ssm_plan(B * H, T, tensor, last), tensor, last);
+    if (n > slots) slots = n;
+  }
+  return align_up(ssm_workspace_bytes(B * H, d_k, d_v, slots));
 }
 
 }  // namespace kata

@@ -35,10 +35,11 @@ __global__ void __launch_bounds__(DV * RG) simt_ssm_kernel(const __grid_constant
   T* op = reinterpret_cast<T*>(a.out.p) + b * a.out.s0 + h * a.out.s1;
   const float A = a.A[h], skip = a.D != nullptr ? a.D[h] : 0.f;
   constexpr size_t SE = (size_t)N * DV;
-  float S[R];
+  float2 S[R / 2];                     // rows rg R + 2 r, + 1
   const float* init = STATE ? nullptr : plan.segments > 1 ? ws + ssm_slot(plan.segments, bh, seg) * SE : a.s_init != nullptr ? a.s_init + (size_t)bh * SE : nullptr;
 #pragma unroll
-  for (int r = 0; r < R; ++r) S[r] = init != nullptr ? init[(rg * R + r) * DV + col] : 0.f;
+  for (int r = 0; r < R / 2; ++r)
+    S[r] = init != nullptr ? make_float2(init[(rg * R + 2 * r) * DV + col], init[(rg * R + 2 * r + 1) * DV + col]) : make_float2(0.f, 0.f);
   Entries<T, E> kr[NQ], qr[NQ], vr[NV];
   float dr = 0.f;
   auto fetch = [&](int t) {
@@ -100,26 +101,22 @@ __global__ void __launch_bounds__(DV * RG) simt_ssm_kernel(const __grid_constant
     }
     __syncthreads();
     if (t + TB < live) fetch(t + TB);
-#pragma unroll 2
+#pragma unroll(R <= 8 ? 8 : R <= 16 ? 4 : 2)
     for (int u = 0; u < TB; ++u) {
-      const float v = vs[u][col], d = as[u];
-      float y = 0.f;
+      const float2 v = make_float2(vs[u][col], vs[u][col]), d = make_float2(as[u], as[u]);
+      float2 y = make_float2(0.f, 0.f);
 #pragma unroll
-      for (int r = 0; r < R; r += 4) {
-        const float4 k4 = *reinterpret_cast<const float4*>(&ks[u][rg * R + r]);
-        S[r] = fmaf(d, S[r], k4.x * v);
-        S[r + 1] = fmaf(d, S[r + 1], k4.y * v);
-        S[r + 2] = fmaf(d, S[r + 2], k4.z * v);
-        S[r + 3] = fmaf(d, S[r + 3], k4.w * v);
+      for (int r = 0; r < R / 2; r += 2) {
+        const float4 k4 = *reinterpret_cast<const float4*>(&ks[u][rg * R + 2 * r]);
+        S[r] = fma_pair(d, S[r], mul_pair(make_float2(k4.x, k4.y), v));
+        S[r + 1] = fma_pair(d, S[r + 1], mul_pair(make_float2(k4.z, k4.w), v));
         if (!STATE) {
-          const float4 q4 = *reinterpret_cast<const float4*>(&qs[u][rg * R + r]);
-          y = fmaf(q4.x, S[r], y);
-          y = fmaf(q4.y, S[r + 1], y);
-          y = fmaf(q4.z, S[r + 2], y);
-          y = fmaf(q4.w, S[r + 3], y);
+          const float4 q4 = *reinterpret_cast<const float4*>(&qs[u][rg * R + 2 * r]);
+          y = fma_pair(make_float2(q4.x, q4.y), S[r], y);
+          y = fma_pair(make_float2(q4.z, q4.w), S[r + 1], y);
         }
       }
-      if (!STATE) part[u][rg][col] = y;
+      if (!STATE) part[u][rg][col] = y.x + y.y;
     }
     if (!STATE) {
       __syncthreads();
@@ -134,7 +131,10 @@ __global__ void __launch_bounds__(DV * RG) simt_ssm_kernel(const __grid_constant
   if constexpr (STATE) {
     float* to = ws + ssm_slot(plan.segments, bh, seg + 1) * SE;
 #pragma unroll
-    for (int r = 0; r < R; ++r) to[(rg * R + r) * DV + col] = S[r];
+    for (int r = 0; r < R / 2; ++r) {
+      to[(rg * R + 2 * r) * DV + col] = S[r].x;
+      to[(rg * R + 2 * r + 1) * DV + col] = S[r].y;
+    }
     if (tid < 32) {
       if (tid >= TB) decay = 0.0;
 #pragma unroll
@@ -145,7 +145,10 @@ __global__ void __launch_bounds__(DV * RG) simt_ssm_kernel(const __grid_constant
     for (int t = max(live, t0) + rg; t < t1; t += RG) op[t * a.out.s2 + col] = from_f32<T>(0.f);
     if (a.s_final != nullptr && seg + 1 == plan.segments) {
 #pragma unroll
-      for (int r = 0; r < R; ++r) a.s_final[(size_t)bh * SE + (rg * R + r) * DV + col] = S[r];
+      for (int r = 0; r < R / 2; ++r) {
+        a.s_final[(size_t)bh * SE + (rg * R + 2 * r) * DV + col] = S[r].x;
+        a.s_final[(size_t)bh * SE + (rg * R + 2 * r + 1) * DV + col] = S[r].y;
+      }
     }
   }
 }
