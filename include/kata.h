@@ -339,7 +339,8 @@ int kata_chunk_state_scan_static(const void* q, const void* k, const void* v, vo
  * R_p turns the pairs (i, i + rotary_dim / 2) (interleaved: (2i, 2i + 1)) of the first rotary_dim entries by p inv_freq[i]
  * radians; the others are left.  The angle is formed as a fraction of a turn in 64-bit integers, exact to 2^-64 p turns, so far
  * positions lose nothing.  Outputs are usually [B,H,T,d], what the attention takes.
- *   d in {16, 32, 64, 128}; rotary_dim a multiple of 16 up to d (0: norm alone); rows 16-byte aligned (KATA_ERR_ALIGNMENT).
+ *   d in {16, 32, 64, 128}; rotary_dim a multiple of 16 up to d (0: norm alone); rows 16-byte aligned (KATA_ERR_ALIGNMENT);
+ *   H_q, H_k <= 32767, B * T <= 2^31 - 1024.
  *   inv_freq: HOST array of rotary_dim / 2 values, read before the call returns.
  *   positions: device int64, position of token (b, t) at b * pos_stride[0] + t * pos_stride[1]; null: pos_offset + t.
  *   q_weight, k_weight: [d] in the element type, or null (ones).  H_k = 0: queries alone.
@@ -370,14 +371,15 @@ int kata_bwd_norm_rope(const kata_norm_rope_args* a, const kata_opts* opts);
 /*
  * Short causal convolution of every channel along the tokens (what the paper's layers put before queries, keys and values):
  *     y_t = act(bias + sum_{j < width} w[j] x_{t - width + 1 + j}),   act(z) = z, or z / (1 + e^-z) with silu
- * x before the first token is zero, or s_init.  width in {2, 3, 4}, any number of channels D; weight [D][width] and bias [D]
- * (or null) contiguous in the element type.
+ * x before the first token is zero, or s_init.  width in {2, 3, 4}, any number of channels D (up to 2^24; T <= 2^30, B T D <= 1e11);
+ * weight [D][width] and bias [D] (or null) contiguous in the element type.
  *   s_init, s_final: [B][D][width - 1] contiguous in the element type, the last width - 1 inputs, oldest first, before the first
  *   token and after the last one of each sequence (either may be null; s_final may be s_init).
  * kata_decode_short_conv: one token, T = 1 (t-strides ignored), s_init and s_final set.
  * kata_bwd_short_conv: dout (read) takes the place of out; writes dx and, where set, dweight [D][width] and dbias [D] (fp32,
  * overwritten, summed in a fixed order).  s_init and s_final must be null: the sequences start at their first token.
- * Rows aligned to 16 bytes (pointers, strides and D) are read 16 bytes at a time, others entry by entry.
+ * Sequences of 32 tokens or more whose rows are whole aligned 16-byte units (pointers, strides and D) go through shared memory,
+ * others from one token to the next in registers, two channels or one at a time: the same sums in the same order.
  * Workspace: kata_workspace_bytes(KATA_FN_BWD_SHORT_CONV, B, D, T, width, 0, 0, opts) for the backward, else none.
  */
 typedef struct kata_short_conv_args {
@@ -404,14 +406,16 @@ int kata_bwd_short_conv(const kata_short_conv_args* a, const kata_opts* opts);
  *     S_t = a_t S_{t-1} + s_t k_t v_t^T,   o_t = S_t^T q_t + D v_t
  * per head, S in R^{n x d_v} in fp32 and in the layout of the first-order state of kata_decode_step.  Queries and keys are
  * shared by the H / G heads of a group (head h reads group h / (H / G)).  n in {16, 32, 64, 128}, d_v in {16, 32, 64}, H a
- * multiple of G, B * H <= 65535; q, k, v, out rows 16-byte aligned.  A, D, dt_bias: [H] fp32; D and dt_bias may be null (0).
+ * multiple of G, B * H <= 65535, T <= 2^30; q, k, v, out rows 16-byte aligned.  A, D, dt_bias: [H] fp32; D and dt_bias may be null (0).
  * dt in the element type, any strides.  A <= 0 and s_t >= 0 are what the recurrence is for: a decay above 1 grows with the
  * distance, and what overflows fp32 on the way is inf or NaN in the result.
  *   s_init, s_final: [B,H,n,d_v] contiguous fp32, 16-byte aligned, the state before the first and after the last token of each
  *   sequence (either may be null; s_final may be s_init).
- * Forms: bf16 with n in {64, 128} and d_v = 64 on the tensor cores (chunks of 128 tokens: the weights inside a chunk and the
- * state that it reads are rounded to bf16, the state that is carried is not); everything else token by token in fp32.  Few heads:
- * the token axis is cut into segments, whose own states come first.
+ * Forms: bf16 with n in {64, 128}, d_v = 64 and more than 32 tokens (with s_final: 64) on the tensor cores, in chunks of 128
+ * tokens: the weights inside a chunk, the values that enter the state which later chunks read, and that state as they read it are
+ * rounded to bf16; s_final is exact to fp32.  Everything else goes token by token in fp32 (impl: KATA_IMPL_TENSOR / KATA_IMPL_SIMT
+ * ask for one form; one row of q, k or v for all tokens, a token stride of 0, is the second's).  Few heads: the token axis is cut into
+ * segments, whose own states come first.
  * Workspace: kata_workspace_bytes(KATA_FN_SSM_SCAN, B, H, T, n, d_v, 0, opts).
  * kata_decode_ssm_step: one token of every head, T = 1 (t-strides ignored, lengths null), s_init = s_final = the state; no workspace.
  */

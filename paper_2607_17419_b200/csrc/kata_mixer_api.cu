@@ -9,6 +9,7 @@ namespace {
 
 constexpr size_t kAlign = 256;
 inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+constexpr int kMaxTokens = 1 << 30;     // of a sequence: token numbers rounded up to whole tiles stay ints
 inline long long elem_bytes(int dtype) { return dtype == KATA_F32 ? 4 : 2; }
 
 // A view that the kernels read 16 bytes at a time: pointer and strides of whole 16-byte units.  Axes of one entry have no stride.
@@ -47,7 +48,7 @@ int norm_rope(const kata_norm_rope_args* a, const kata_opts* opts, bool backward
   if (a == nullptr || a->struct_size != sizeof(kata_norm_rope_args)) return KATA_ERR_INVALID_ARG;
   if (a->B < 1 || a->T < 1 || a->H_q < 1 || a->H_k < 0 || a->d < 1 || a->rotary_dim < 0) return KATA_ERR_INVALID_ARG;
   if (!rope_width(a->d) || a->rotary_dim > a->d || a->rotary_dim % 16 != 0) return KATA_ERR_UNSUPPORTED_SHAPE;
-  // (a row has at most 32 lanes, and the grid's axes are 32-bit)
+  // (tokens are numbered in 32 bits, heads of q and k together in 16)
   if (a->H_q > 32767 || a->H_k > 32767 || (long long)a->B * a->T > (1LL << 31) - 1024) return KATA_ERR_UNSUPPORTED_SHAPE;
   if (o.impl == KATA_IMPL_TENSOR) return KATA_ERR_UNSUPPORTED_SHAPE;
   if (!(a->eps >= 0.0) || !std::isfinite(a->eps) || (a->rotary_dim > 0 && a->inv_freq == nullptr)) return KATA_ERR_INVALID_ARG;
@@ -107,8 +108,8 @@ int short_conv(const kata_short_conv_args* a, const kata_opts* opts, ConvCall ca
   const int T = call == kConvStep ? 1 : a->T;
   if (a->B < 1 || T < 1 || a->D < 1 || a->width < 1) return KATA_ERR_INVALID_ARG;
   if (a->width < 2 || a->width > 4) return KATA_ERR_UNSUPPORTED_SHAPE;
-  // (threads are numbered over tokens x channels in at most 2^31 blocks)
-  if (a->D > (1 << 24) || (double)a->B * T * a->D > 1e11) return KATA_ERR_UNSUPPORTED_SHAPE;
+  // (at most 2^31 blocks over tokens x channels)
+  if (T > kMaxTokens || a->D > (1 << 24) || (double)a->B * T * a->D > 1e11) return KATA_ERR_UNSUPPORTED_SHAPE;
   if (o.impl == KATA_IMPL_TENSOR) return KATA_ERR_UNSUPPORTED_SHAPE;
   if (a->weight == nullptr) return KATA_ERR_INVALID_ARG;
   if (call == kConvStep && (a->s_init == nullptr || a->s_final == nullptr || a->lengths != nullptr)) return KATA_ERR_INVALID_ARG;
@@ -148,7 +149,7 @@ int short_conv(const kata_short_conv_args* a, const kata_opts* opts, ConvCall ca
 
 int ssm_shape(int B, int H, int T, int n, int d) {
   if (B < 1 || H < 1 || T < 1 || n < 1 || d < 1) return KATA_ERR_INVALID_ARG;
-  if ((long long)B * H > 65535) return KATA_ERR_UNSUPPORTED_SHAPE;
+  if ((long long)B * H > 65535 || T > kMaxTokens) return KATA_ERR_UNSUPPORTED_SHAPE;
   if ((n != 16 && n != 32 && n != 64 && n != 128) || (d != 16 && d != 32 && d != 64)) return KATA_ERR_UNSUPPORTED_SHAPE;
   return KATA_OK;
 }
@@ -218,9 +219,10 @@ int ssm(const kata_ssm_args* a, const kata_opts* opts, bool step) {
 size_t mixer_workspace_bytes(int fn, int B, int H, int T, int d_k, int d_v, const kata_opts* opts) {
   CallOpts o;
   if (read_call_opts(opts, o) != KATA_OK || B < 1 || H < 1 || T < 1) return 0;
+  if (fn == KATA_FN_BWD_NORM_ROPE && (H > 65534 || (long long)B * T > (1LL << 31) - 1024)) return 0;
   if (fn == KATA_FN_BWD_NORM_ROPE) return rope_width(d_k) ? align_up(norm_rope_bwd_workspace_elems(B, T, H, d_k) * sizeof(float)) : 0;
   if (fn == KATA_FN_BWD_SHORT_CONV)
-    return d_k >= 2 && d_k <= 4 && H <= (1 << 24) && (double)B * T * H <= 1e11 ? align_up(short_conv_bwd_workspace_elems(B, T, H, d_k) * sizeof(float)) : 0;
+    return d_k >= 2 && d_k <= 4 && T <= kMaxTokens && H <= (1 << 24) && (double)B * T * H <= 1e11 ? align_up(short_conv_bwd_workspace_elems(B, T, H, d_k) * sizeof(float)) : 0;
   if (ssm_shape(B, H, T, d_k, d_v) != KATA_OK) return 0;
   // (what a call with or without a final state takes)
   int slots = 0;

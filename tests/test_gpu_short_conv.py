@@ -117,3 +117,27 @@ def test_offsets_beyond_32_bits():
     v.copy_(torch.randn(2, 8, 64, device="cuda"))
     w = torch.randn(64, 4, device="cuda").bfloat16()
     assert torch.equal(kb.kata_fwd_short_conv(v, w, silu=True), kb.kata_fwd_short_conv(v.contiguous(), w, silu=True))
+
+
+@pytest.mark.parametrize("T,D", [(5, 64), (200, 64), (200, 63)])
+def test_broadcast_and_shifted_views(T, D):
+    """One sequence for all of a batch, and rows that begin at any entry: the same sums whatever path reads them."""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    n = lambda *s: torch.randn(*s, device="cuda", generator=gen).bfloat16()
+    x, w, b, g = n(1, T, D), n(D, 4), n(D), n(3, T, D)
+    wide = x.expand(3, -1, -1)
+    want = kb.kata_fwd_short_conv(wide.contiguous(), w, b, silu=True)
+    assert torch.equal(kb.kata_fwd_short_conv(wide, w, b, silu=True), want)
+    grads = kb.kata_bwd_short_conv(g, wide.contiguous(), w, b, silu=True)
+    assert all(torch.equal(p, q) for p, q in zip(kb.kata_bwd_short_conv(g, wide, w, b, silu=True), grads))
+    for shift in (1, 2, 8):
+        room = n(3, T, D + 16)
+        room[..., shift:shift + D] = x
+        y = kb.kata_fwd_short_conv(room[..., shift:shift + D], w, b, silu=True)
+        dx, dw, db = kb.kata_bwd_short_conv(g, room[..., shift:shift + D], w, b, silu=True)
+        assert torch.equal(y, want) and torch.equal(dx, grads[0])
+        # (the same 3 T terms summed in another order: 3 T roundings on each side of sums no larger than the terms' sizes, SiLU's slope
+        # at most 1.1; a shifted sum of products is at most the product of the norms)
+        sizes = (1.1 * g.double().norm(dim=(0, 1)) * (3.0 ** 0.5) * x.double().norm(dim=(0, 1)), 1.1 * g.double().abs().sum((0, 1)))
+        for p, q, size in ((dw, grads[1], sizes[0][:, None]), (db, grads[2], sizes[1])):
+            assert torch.all((p - q).abs() <= 2 * 3 * T * F32 * size)

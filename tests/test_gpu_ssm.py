@@ -148,3 +148,67 @@ def test_misaligned_rows_are_refused():
     x = torch.zeros(2 * 20 * 64 + 8, device="cuda", dtype=torch.bfloat16)
     with pytest.raises(kb.KataError):
         kb.kata_fwd_ssm_scan(q, k, x[1:1 + 2 * 20 * 64].view(1, 2, 20, 64), dt, A)
+
+
+@pytest.mark.parametrize("dtype,n", [("bf16", 64), ("bf16", 128), ("f32", 16)])
+def test_broadcast_views(dtype, n):
+    """Queries, keys and values shared by batches, heads or tokens (strides of 0) are what their copies are."""
+    B, H, G, T, d = 3, 4, 2, 140, 64
+    q, k, v, dt, A, D, bias, _, _ = tensors(dtype, B, H, G, T, n, d, 13, packed=False)
+    cases = [(q[:1].expand(B, -1, -1, -1), k[:, :1].expand(-1, G, -1, -1), v), (q[:1, :1].expand(B, G, -1, -1), k, v[:, :1].expand(-1, H, -1, -1)),
+             (q, k, v[:1].expand(B, -1, -1, -1))]
+    for a, b, c in cases:
+        got = kb.kata_fwd_ssm_scan(a, b, c, dt, A, D, bias, dt_softplus=True)
+        assert torch.equal(got, kb.kata_fwd_ssm_scan(a.contiguous(), b.contiguous(), c.contiguous(), dt, A, D, bias, dt_softplus=True))
+    # one key for all tokens: token by token
+    one = k[:, :, :1].expand(-1, -1, T, -1)
+    S, S2 = torch.empty(B, H, n, d, device="cuda"), torch.empty(B, H, n, d, device="cuda")
+    got = kb.kata_fwd_ssm_scan(q, one, v, dt, A, D, bias, dt_softplus=True, s_final=S)
+    assert kb.kata_last_impl() == kb.KATA_IMPL_SIMT
+    want = kb.kata_fwd_ssm_scan(q, one.contiguous(), v, dt, A, D, bias, dt_softplus=True, s_final=S2, impl=kb.KATA_IMPL_SIMT)
+    assert torch.equal(got, want) and torch.equal(S, S2)
+    if dtype == "bf16":
+        with pytest.raises(kb.KataError):
+            kb.kata_fwd_ssm_scan(q, one, v, dt, A, D, bias, dt_softplus=True, impl=kb.KATA_IMPL_TENSOR)
+
+
+def test_outputs_of_any_layout():
+    """Outputs into a view of a larger tensor: its other entries stay."""
+    B, H, T, d = 2, 4, 200, 64
+    q, k, v, dt, A, D, bias, _, _ = tensors("bf16", B, H, 1, T, 64, d, 15)
+    want = kb.kata_fwd_ssm_scan(q, k, v, dt, A, D, bias, dt_softplus=True)
+    room = torch.full((B, T + 3, H, 2 * d), 7.0, device="cuda", dtype=torch.bfloat16)
+    view = room[:, 1:T + 1, :, d:].transpose(1, 2)
+    for lengths in (None, torch.tensor([5, 150], dtype=torch.int32, device="cuda")):
+        room.fill_(7.0)
+        got = kb.kata_fwd_ssm_scan(q, k, v, dt, A, D, bias, dt_softplus=True, lengths=lengths, out=view)
+        assert got.data_ptr() == view.data_ptr()
+        if lengths is None:
+            assert torch.equal(view, want)
+        else:
+            assert all(torch.equal(view[b, :, :n], want[b, :, :n]) and torch.all(view[b, :, n:] == 0) for b, n in enumerate(lengths.tolist()))
+        assert torch.all(room[:, 0] == 7) and torch.all(room[:, T + 1:] == 7) and torch.all(room[..., :d] == 7)
+
+
+@pytest.mark.parametrize("T", [1, 31, 32, 33, 64, 65, 127, 128, 129, 255, 257])
+def test_lengths_at_the_borders(T):
+    """Around the rules' and the tiles' borders, with and without a final state."""
+    q, k, v, dt, A, D, bias, init, _ = tensors("bf16", 2, 2, 1, T, 64, 64, 17)
+    ref = ssm(q, k, v, dt, A, D, bias, True, init)
+    S = init.clone()
+    check(kb.kata_fwd_ssm_scan(q, k, v, dt, A, D, bias, dt_softplus=True, s_init=S, s_final=S), S, ref, "bf16", T, 64, True)
+    check(kb.kata_fwd_ssm_scan(q, k, v, dt, A, D, bias, dt_softplus=True, s_init=init), None, ref, "bf16", T, 64, True)
+
+
+def test_steep_and_flat_decays():
+    """Heads that forget everything within a token, nothing, and what lies between, on both forms."""
+    B, H, T = 1, 6, 300
+    q, k, v, _, _, D, _, init, _ = tensors("bf16", B, H, 1, T, 64, 64, 19)
+    dt = torch.rand(B, H, T, device="cuda").bfloat16()
+    dt[:, :, 40:44] = 0
+    A = torch.tensor([-1000.0, -30.0, -8.0, -5.0, -1e-4, 0.0], device="cuda")
+    ref = ssm(q, k, v, dt, A, D, init=init)
+    for impl in (0, 1):
+        S = init.clone()
+        out = kb.kata_fwd_ssm_scan(q, k, v, dt, A, D, s_init=S, s_final=S, impl=impl)
+        check(out, S, ref, "bf16", T, 64, impl == 0)

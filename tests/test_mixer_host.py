@@ -73,7 +73,7 @@ def test_norm_rope_arguments(L, fn):
     nan = rope()
     nan.keep[3] = float("nan")
     assert call(L, fn, nan, o()) == INV
-    for bad in (dict(d=48), dict(d=256), dict(rotary_dim=8), dict(rotary_dim=80), dict(rotary_dim=128)):
+    for bad in (dict(d=48), dict(d=256), dict(rotary_dim=8), dict(rotary_dim=80), dict(rotary_dim=128), dict(H_q=32768), dict(B=1 << 20, T=1 << 11)):
         assert call(L, fn, rope(**bad), o()) == SHAPE, bad
     for bad in (dict(q=P + 8), dict(k_out=P + 2), dict(q_stride=(1280, 324, 64)), dict(k_stride=(1280, 320, 65)), dict(q_weight=P + 1), dict(positions=P + 4)):
         assert call(L, fn, rope(**bad), o()) == ALIGN, bad
@@ -151,7 +151,7 @@ def test_ssm_arguments(L, fn):
     for bad in (dict(struct_size=8), dict(B=0), dict(H=0), dict(G=0), dict(G=3), dict(n=0), dict(q=None), dict(k=None), dict(v=None), dict(dt=None),
                 dict(out=None), dict(A=None), dict(dt_stride=(-20, 5, 1)), dict(out_stride=(0, 320, 64)), dict(out_stride=(1280, 0, 64))):
         assert call(L, fn, ssm(**bad), o()) == INV, bad
-    for bad in (dict(n=48), dict(n=256), dict(d_v=128), dict(d_v=8), dict(B=65536, H=2)):
+    for bad in (dict(n=48), dict(n=256), dict(d_v=128), dict(d_v=8), dict(B=65536, H=2)) + ((dict(T=(1 << 30) + 1),) if fn == "kata_fwd_ssm_scan" else ()):
         assert call(L, fn, ssm(**bad), o()) == SHAPE, bad
     for bad in (dict(q=P + 8), dict(v_stride=(1280, 321, 64)), dict(out=P + 4), dict(dt=P + 1), dict(A=P + 2), dict(s_init=P + 8, s_final=P + 8)):
         assert call(L, fn, ssm(**bad), o()) == ALIGN, bad
@@ -236,3 +236,16 @@ CALLS = dict(refused_calls())
 def test_refused(name):
     with pytest.raises(ValueError):
         CALLS[name]()
+
+
+def test_no_unbounded_wait_between_the_warps():
+    """The scan's tensor-core kernels meet at barriers with a bounded wait and at __syncthreads behind all roles, nowhere else."""
+    text = open(os.path.join(ROOT, "paper_2607_17419_b200", "csrc", "kata_tc_ssm.cu")).read()
+    assert not re.search(r"\bbar(rier)?\.(cta\.)?(sync|red)|named_barrier|__nanosleep|while \(", text)
+    for role in re.split(r"// =+ ", text)[1:]:
+        assert "__syncthreads" not in role.split("// ---------------- teardown")[0]
+    # no sum across lanes stands in one side of a choice (a lane that does not take part is waited for without a limit)
+    for name in ("kata_norm_rope.cu", "kata_short_conv.cu", "kata_simt_ssm.cu", "kata_ssm_step.cu", "kata_tc_ssm.cu"):
+        for line in open(os.path.join(ROOT, "paper_2607_17419_b200", "csrc", name)):
+            code = line.split("//")[0]
+            assert not re.search(r"\?.*(row_sum|_sync)\s*\(", code), (name, line)
