@@ -318,7 +318,7 @@ void ssm_step(const Ssm& a, LaunchCtx& ctx);
 struct SsmPlan {
   int segments, seg_tokens;
 };
-SsmPlan ssm_plan(int BH, int T, bool tensor, bool final_state);
+SsmPlan ssm_plan(int BH, int T, int n, int d, bool tensor, bool final_state);
 size_t ssm_workspace_bytes(int BH, int n, int d, int slots);
 void ssm_prefix(const Ssm& a, const SsmPlan& plan, int slots, float* ws, LaunchCtx& ctx);
 void simt_ssm(const Ssm& a, const SsmPlan& plan, float* ws, LaunchCtx& ctx);

@@ -198,7 +198,7 @@ int ssm(const kata_ssm_args* a, const kata_opts* opts, bool step) {
   for (const void* p : {(const void*)a->A, (const void*)a->D, (const void*)a->dt_bias, (const void*)a->lengths})
     if ((reinterpret_cast<uintptr_t>(p) & 3u) != 0) return KATA_ERR_ALIGNMENT;
   if ((reinterpret_cast<uintptr_t>(a->s_init) & 15u) != 0 || (reinterpret_cast<uintptr_t>(a->s_final) & 15u) != 0) return KATA_ERR_ALIGNMENT;
-  const SsmPlan plan = step ? SsmPlan{1, 1} : ssm_plan(a->B * a->H, T, tensor, r.s_final != nullptr);
+  const SsmPlan plan = step ? SsmPlan{1, 1} : ssm_plan(a->B * a->H, T, a->n, a->d_v, tensor, r.s_final != nullptr);
   if (tensor && T > 1 && (r.q.s2 == 0 || r.k.s2 == 0 || r.v.s2 == 0)) {      // (one row for all tokens has no tensor map)
     if (o.impl == KATA_IMPL_TENSOR) return KATA_ERR_UNSUPPORTED_SHAPE;
     tensor = false;
@@ -228,7 +228,7 @@ size_t mixer_workspace_bytes(int fn, int B, int H, int T, int d_k, int d_v, cons
   int slots = 0;
   for (const bool last : {false, true}) {
     const bool tensor = ssm_tensor(o, d_k, d_v, T, last);
-    const int n = ssm_slots(ssm_plan(B * H, T, tensor, last), tensor, last);
+    const int n = ssm_slots(ssm_plan(B * H, T, d_k, d_v, tensor, last), tensor, last);
     if (n > slots) slots = n;
   }
   return align_up(ssm_workspace_bytes(B * H, d_k, d_v, slots));

@@ -89,8 +89,9 @@ __device__ __forceinline__ float2 add_pair(float2 a, float2 b) {
 
 // Launches with programmatic stream serialisation: the kernel may become resident before the one ahead of it in the stream has
 // ended, and waits for it (cudaGridDependencySynchronize) before it touches memory.
+// early = false: it starts when that kernel has ended.
 template <typename... P, typename... A>
-inline void launch_after(LaunchCtx& ctx, void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, A&&... args) {
+inline void launch_when(bool early, LaunchCtx& ctx, void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, A&&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = block;
@@ -100,7 +101,7 @@ inline void launch_after(LaunchCtx& ctx, void (*kernel)(P...), dim3 grid, dim3 b
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = early ? 1 : 0;
   if (ctx.status != KATA_OK) return;
   if (cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) != cudaSuccess) {
     cudaGetLastError();
@@ -108,6 +109,11 @@ inline void launch_after(LaunchCtx& ctx, void (*kernel)(P...), dim3 grid, dim3 b
     return;
   }
   ++ctx.launches;
+}
+
+template <typename... P, typename... A>
+inline void launch_after(LaunchCtx& ctx, void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, A&&... args) {
+  launch_when(true, ctx, kernel, grid, block, smem, args...);
 }
 
 __device__ __forceinline__ void wait_for_kernels_ahead() {

@@ -638,16 +638,18 @@ struct ConvGrid {
   dim3 block;
   long long row_blocks;
 };
-// Segments of 64 tokens; shorter ones (down to 8) while there are fewer threads than the GPU holds.
-ConvGrid conv_grid(int B, int T, int D, int vec) {
+// Segments of 32 tokens; shorter ones (down to 8, backward 16: its sums are per segment) while there are fewer threads than the GPU
+// holds.  Measured, us, bf16, segments of 8 / 16 / 32 / 64: 1 x 4096 x 1000 channels forward 6.1 / 6.7 / 8.0 / 8.8, backward 24.4 / 20.2 /
+// 25.6 / 36.3; 8 x 4096 x 1000 forward 44.5 / 41.0 / 39.2 / 46.2, backward 192 / 147 / 124 / 131.
+ConvGrid conv_grid(int B, int T, int D, int vec, bool backward) {
   ConvGrid g;
   g.groups = (D + vec - 1) / vec;
   int tx = 1;
   while (tx < g.groups && tx < 64) tx *= 2;
   g.block = dim3(tx, kThreads / tx);
   g.col_blocks = (g.groups + tx - 1) / tx;
-  g.seg_tokens = 64;
-  while (g.seg_tokens > 8 && (double)g.groups * B * ((T + g.seg_tokens - 1) / g.seg_tokens) < kPlanSMs * 1024.0) g.seg_tokens /= 2;
+  g.seg_tokens = 32;
+  while (g.seg_tokens > (backward ? 16 : 8) && (double)g.groups * B * ((T + g.seg_tokens - 1) / g.seg_tokens) < kPlanSMs * 1024.0) g.seg_tokens /= 2;
   g.segs = (T + g.seg_tokens - 1) / g.seg_tokens;
   g.row_blocks = ((long long)B * g.segs + g.block.y - 1) / g.block.y;
   return g;
@@ -682,12 +684,19 @@ TileGrid tile_grid(int B, int T, int D, int elem, int run) {
   if (g.walkers > 65535) g.walkers = 65535;
   return g;
 }
-// Rows of whole 16-byte units; a tile has to be worth its start (measured, us, walk / tiles, 16 x 1024 channels: T = 1: 2.6 / 3.3).
-bool tiled(const ShortConv& a, const View& v) { return conv_aligned(a, v, 16); }
+// Tiles need rows of whole 16-byte units and, so that they are worth their start and are not mostly empty, sizes of these rules.
+// Measured, us, walk / tiles, T x 1024 channels of 32768 tokens unless others are named:
+//   forward, bf16: T = 64: 47 / 49, 128: 48 / 27, 16384: 47 / 27; 4096 tokens: 6.8 / 6.3, 1024 tokens: 3.8 / 4.4
+//   forward, fp32: T = 64: 66 / 90, 128: 66 / 48; 8192 tokens: 17.5 / 16.4, 4096 tokens: 9.4 / 10.8
+//   backward, bf16, 16384 tokens: T = 32: 72 / 95, 64: 72 / 62, 128: 72 / 52; 8192 tokens (two rounds of tiles begun): 41 / 32, 4096 (two, the
+//   second nearly empty): 20 / 24, 2048 (one): 15.8 / 15.2.  Backward in fp32: 104 / 110, 189 / 209 of 32768 tokens: never.
 bool use_tiles(const ShortConv& a, bool backward) {
   const int e = a.dtype == KATA_F32 ? 4 : 2;
-  if (a.T < 32 || (a.D * e) % 16 != 0 || !tiled(a, a.x)) return false;
-  return !backward || tiled(a, a.dout);
+  if ((a.D * e) % 16 != 0 || !conv_aligned(a, a.x, 16)) return false;
+  if (!backward) return a.T >= 128 && (double)a.B * a.T * a.D >= (e == 2 ? 1 << 21 : 1 << 23);
+  if (e != 2 || a.T < 64 || !conv_aligned(a, a.dout, 16)) return false;
+  const TileGrid g = tile_grid(a.B, a.T, a.D, e, kBwdRun);
+  return g.n_tiles <= g.walkers || g.n_tiles >= 2 * g.walkers;
 }
 
 template <typename T, int W, bool SILU> void launch_tiles(const ShortConv& a, LaunchCtx& ctx) {
@@ -714,12 +723,12 @@ template <typename T, int W, bool SILU> void launch_bwd_tiles(const ShortConv& a
 }
 
 template <typename T, int W, int VEC> void launch_fwd(const ShortConv& a, LaunchCtx& ctx) {
-  const ConvGrid g = conv_grid(a.B, a.T, a.D, VEC);
+  const ConvGrid g = conv_grid(a.B, a.T, a.D, VEC, false);
   launch_after(ctx, short_conv_kernel<T, W, VEC>, dim3((unsigned)(g.row_blocks * g.col_blocks)), g.block, 0, a, g.groups, g.col_blocks, g.segs, g.seg_tokens, taps_aligned(a));
 }
 
 template <typename T, int W, int VEC> void launch_bwd(const ShortConv& a, float* ws, LaunchCtx& ctx) {
-  const ConvGrid g = conv_grid(a.B, a.T, a.D, VEC);
+  const ConvGrid g = conv_grid(a.B, a.T, a.D, VEC, true);
   const bool sums = a.dweight != nullptr || a.dbias != nullptr;
   const size_t smem = sums ? (size_t)kThreads * VEC * (W + 1) * sizeof(float) : 0;
   launch_after(ctx, short_conv_bwd_kernel<T, W, VEC>, dim3((unsigned)(g.row_blocks * g.col_blocks)), g.block, smem, a, g.groups, g.col_blocks, g.segs,
@@ -734,8 +743,10 @@ template <typename T, int W> void dispatch(const ShortConv& a, bool backward, fl
   constexpr int bytes = kVec * sizeof(T);
   if (backward) {
     const bool pairs = a.D % kVec == 0 && conv_aligned(a, a.dx, bytes);
-    if (pairs && use_tiles(a, true)) a.silu ? launch_bwd_tiles<T, W, true>(a, ws, ctx) : launch_bwd_tiles<T, W, false>(a, ws, ctx);
-    else if (pairs && conv_aligned(a, a.x, bytes) && conv_aligned(a, a.dout, bytes)) launch_bwd<T, W, kVec>(a, ws, ctx);
+    if constexpr (sizeof(T) == 2) {
+      if (pairs && use_tiles(a, true)) return a.silu ? launch_bwd_tiles<T, W, true>(a, ws, ctx) : launch_bwd_tiles<T, W, false>(a, ws, ctx);
+    }
+    if (pairs && conv_aligned(a, a.x, bytes) && conv_aligned(a, a.dout, bytes)) launch_bwd<T, W, kVec>(a, ws, ctx);
     else launch_bwd<T, W, 1>(a, ws, ctx);
   } else {
     const bool pairs = a.D % kVec == 0 && conv_aligned(a, a.out, bytes);
@@ -763,8 +774,8 @@ void short_conv_fwd(const ShortConv& a, LaunchCtx& ctx) { run(a, false, nullptr,
 
 // (the most of all ways to read rows: the scratch depends on sizes alone)
 size_t short_conv_bwd_workspace_elems(int B, int T, int D, int W) {
-  long long most = conv_grid(B, T, D, 1).row_blocks;
-  const long long others[3] = {conv_grid(B, T, D, kVec).row_blocks, tile_grid(B, T, D, 2, kBwdRun).walkers, tile_grid(B, T, D, 4, kBwdRun).walkers};
+  long long most = conv_grid(B, T, D, 1, true).row_blocks;
+  const long long others[2] = {conv_grid(B, T, D, kVec, true).row_blocks, tile_grid(B, T, D, 2, kBwdRun).walkers};
   for (const long long o : others)
     if (o > most) most = o;
   return (size_t)most * (W + 1) * D;

@@ -2,7 +2,8 @@
 //   S <- a_t S + s_t k_t v_t^T,  o_t = S^T q_t + D v_t
 // One CTA per head and segment of the tokens, the state in registers: a thread has one column and a quarter of the rows.  Tokens are
 // staged 16 at a time (s_t folded into the keys), the next 16 on their way meanwhile; the four sums of an output meet in shared
-// memory.  Bound by fp32 issue: three operations per state entry and token.
+// memory.  Bound by fp32 issue: three operations per state entry and token. n = d_v = 64, fp32: 17.6 us for 128 tokens of one head alone on an SM
+// (latency), 13 us a head where an SM has several; fp32, 128 heads x 2000 tokens: 281 us.
 // Few heads: the token axis is cut into segments.  Their own states (from zero) come first, ssm_prefix turns them into the states
 // before the segments, and the second pass starts from those.
 #include <cmath>
@@ -183,11 +184,15 @@ __global__ void __launch_bounds__(128) ssm_prefix_kernel(float* __restrict__ ws,
 
 template <typename T, int N, int DV> void launch(const Ssm& a, const SsmPlan& plan, float* ws, LaunchCtx& ctx) {
   const dim3 grid((unsigned)(a.B * a.H) * plan.segments);
+  // A CTA that is resident early has to take the SM that is left: behind ssm_prefix, or another kernel of many CTAs, some SMs then get
+  // several of these and others none.  (fp32, n = d_v = 64, 16 heads x 1000 tokens: 43.6 us early, 29.4 us not; 256 heads x 512 tokens: 154 and
+  // 115.  Short calls gain a little by being there: 2 heads x 512, n = d_v = 16: 8.9 and 9.8, 16 heads x 40: 9.2 and 9.3.)
+  const bool early = a.T <= 64;
   if (plan.segments > 1) {
-    launch_after(ctx, simt_ssm_kernel<T, N, DV, true>, grid, dim3(DV * RG), 0, a, plan, ws);
+    launch_when(early, ctx, simt_ssm_kernel<T, N, DV, true>, grid, dim3(DV * RG), 0, a, plan, ws);
     ssm_prefix(a, plan, plan.segments, ws, ctx);
   }
-  launch_after(ctx, simt_ssm_kernel<T, N, DV, false>, grid, dim3(DV * RG), 0, a, plan, ws);
+  launch_when(early, ctx, simt_ssm_kernel<T, N, DV, false>, grid, dim3(DV * RG), 0, a, plan, ws);
 }
 
 template <typename T, int N> void by_width(const Ssm& a, const SsmPlan& plan, float* ws, LaunchCtx& ctx) {
@@ -205,21 +210,28 @@ template <typename T> void by_rows(const Ssm& a, const SsmPlan& plan, float* ws,
 
 }  // namespace
 
-// Segments of whole 128-token tiles.  The passes take whole waves of CTAs (one per SM on the tensor cores, four of the token by token
-// kernel); several segments, and a final state on the tensor cores, take the pass of the states too.  The number of segments with the
-// smallest sum.  Measured, us a tile, outputs and states: tensor cores 1.85 and 0.75 (n = 64), token by token 8 and 6.5.
-SsmPlan ssm_plan(int BH, int T, bool tensor, bool final_state) {
-  const int tiles = (T + 127) / 128, resident = kPlanSMs * (tensor ? 1 : 4);
-  const double out_us = tensor ? 1.85 : 8.0, state_us = tensor ? 0.75 : 6.5;
-  SsmPlan best{1, tiles * 128};
+// Segments of whole tiles (128 tokens on the tensor cores, else 32) and how long a pass takes by the rates measured here: a tile of
+// the outputs and one of the states, in us, times the CTAs that an SM has in a row.  On the tensor cores an SM has one CTA; of the
+// token by token kernel it runs 1.25 of 256 threads (2.5 of 128, 5 of 64) as fast as one.  Several segments, and a final state on the
+// tensor cores, take the pass of the states too.  The smallest sum wins; more CTAs than eight per SM never did.  Measured, us with one
+// segment / two / this rule's: fp32, n = d_v = 64, 16 heads x 1000 tokens: 142 / 118 / 29; bf16, n = d_v = 16, 16 heads x 16384: 1320 /
+// 1035 / 58; fp32, n = d_v = 64, 128 heads x 2000 (the rule stays with one): 281 / 350 / 281.
+SsmPlan ssm_plan(int BH, int T, int n, int d, bool tensor, bool final_state) {
+  const int tile = tensor ? 128 : 32, tiles = (T + tile - 1) / tile;
+  const double out_us = tensor ? 1.85 : 2.0 + 0.039 * n, state_us = tensor ? 0.75 : 0.6 * out_us;
+  const double together = tensor ? 1.0 : 80.0 / d;
+  const long long most = kPlanSMs * (tensor ? 2LL : 8LL);
+  SsmPlan best{1, tiles * tile};
   double best_us = 0.0;
-  for (int want = 1; want <= tiles && (want == 1 || (long long)BH * (want - 1) < 2LL * resident); ++want) {
-    const int per = (tiles + want - 1) / want, n = (tiles + per - 1) / per;
-    const bool states = n > 1 || (tensor && final_state);
-    const double us = ceil((double)BH * n / resident) * per * (out_us + (states ? state_us : 0.0)) + (states ? 8.0 + 0.1 * n : 0.0);
+  for (int want = 1; want <= tiles && (want == 1 || (long long)BH * (want - 1) < most); ++want) {
+    const int per = (tiles + want - 1) / want, segments = (tiles + per - 1) / per;
+    const bool states = segments > 1 || (tensor && final_state);
+    const long long row = ((long long)BH * segments + kPlanSMs - 1) / kPlanSMs;
+    const double us = (row > together ? row / together : 1.0) * per * (out_us + (states ? state_us : 0.0)) +
+                      (states ? (tensor ? 8.0 + 0.1 * segments : 3.0 + 0.07 * segments) : 0.0);
     if (want == 1 || us < best_us) {
       best_us = us;
-      best = SsmPlan{n, per * 128};
+      best = SsmPlan{segments, per * tile};
     }
   }
   return best;

@@ -141,3 +141,33 @@ def test_broadcast_and_shifted_views(T, D):
         sizes = (1.1 * g.double().norm(dim=(0, 1)) * (3.0 ** 0.5) * x.double().norm(dim=(0, 1)), 1.1 * g.double().abs().sum((0, 1)))
         for p, q, size in ((dw, grads[1], sizes[0][:, None]), (db, grads[2], sizes[1])):
             assert torch.all((p - q).abs() <= 2 * 3 * T * F32 * size)
+
+
+LARGE = [  # sizes whose forward goes through shared memory: dtype, B, T, D, W, silu, bias, extra columns of the rows
+    ("bf16", 5, 500, 1024, 4, True, True, 0), ("bf16", 2, 1100, 1032, 3, False, False, 8), ("bf16", 130, 129, 136, 2, True, True, 0),
+    ("bf16", 3, 40000, 24, 4, True, True, 0), ("f32", 3, 2801, 1004, 4, True, True, 4),
+]
+
+
+@pytest.mark.parametrize("dtype,B,T,D,W,silu,bias,extra", LARGE)
+@pytest.mark.parametrize("state,padded", [(False, False), (True, True)])
+def test_large_forward(dtype, B, T, D, W, silu, bias, extra, state, padded):
+    test_forward(dtype, B, T, D, W, silu, bias, extra, state, padded)
+
+
+@pytest.mark.parametrize("dtype,B,T,D,W,silu,bias,extra", LARGE[:3])
+@pytest.mark.parametrize("padded", [False, True])
+def test_large_backward(dtype, B, T, D, W, silu, bias, extra, padded):
+    test_backward(dtype, B, T, D, W, silu, bias, extra, padded)
+
+
+@pytest.mark.parametrize("T,D", [(300, 4096), (70, 64)])
+def test_long_sequences_beyond_32_bits(T, D):
+    x = torch.empty((1 << 31) + T * D, device="cuda", dtype=torch.bfloat16)
+    v = torch.as_strided(x, (2, T, D), (1 << 31, D, 1))
+    v.copy_(torch.randn(2, T, D, device="cuda"))
+    w, g = torch.randn(D, 4, device="cuda").bfloat16(), torch.randn(2, T, D, device="cuda").bfloat16()
+    assert torch.equal(kb.kata_fwd_short_conv(v, w, silu=True), kb.kata_fwd_short_conv(v.contiguous(), w, silu=True))
+    for a, b in ((v, v.contiguous()), (g, g)):
+        assert all(p is q or torch.equal(p, q) for p, q in zip(kb.kata_bwd_short_conv(g, a, w, silu=True), kb.kata_bwd_short_conv(g, b, w, silu=True)))
+    assert torch.equal(kb.kata_bwd_short_conv(v, g, w, silu=True)[0], kb.kata_bwd_short_conv(v.contiguous(), g, w, silu=True)[0])
