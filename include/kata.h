@@ -378,8 +378,8 @@ int kata_bwd_norm_rope(const kata_norm_rope_args* a, const kata_opts* opts);
  * kata_decode_short_conv: one token, T = 1 (t-strides ignored), s_init and s_final set.
  * kata_bwd_short_conv: dout (read) takes the place of out; writes dx and, where set, dweight [D][width] and dbias [D] (fp32,
  * overwritten, summed in a fixed order).  s_init and s_final must be null: the sequences start at their first token.
- * Sequences of 32 tokens or more whose rows are whole aligned 16-byte units (pointers, strides and D) go through shared memory,
- * others from one token to the next in registers, two channels or one at a time: the same sums in the same order.
+ * Large enough calls whose rows are whole aligned 16-byte units (pointers, strides and D) go through shared memory, others from one
+ * token to the next in registers, two channels or one at a time: out and dx are the same sums in the same order.
  * Workspace: kata_workspace_bytes(KATA_FN_BWD_SHORT_CONV, B, D, T, width, 0, 0, opts) for the backward, else none.
  */
 typedef struct kata_short_conv_args {
@@ -415,7 +415,8 @@ int kata_bwd_short_conv(const kata_short_conv_args* a, const kata_opts* opts);
  * tokens: the weights inside a chunk, the values that enter the state which later chunks read, and that state as they read it are
  * rounded to bf16; s_final is exact to fp32.  Everything else goes token by token in fp32 (impl: KATA_IMPL_TENSOR / KATA_IMPL_SIMT
  * ask for one form; one row of q, k or v for all tokens, a token stride of 0, is the second's).  Few heads: the token axis is cut into
- * segments, whose own states come first.
+ * segments, whose own states come first.  A NaN or infinity in a live token reaches, beside what follows it, the outputs of its own
+ * chunk on the tensor cores (a weight of 0 times it).
  * Workspace: kata_workspace_bytes(KATA_FN_SSM_SCAN, B, H, T, n, d_v, 0, opts).
  * kata_decode_ssm_step: one token of every head, T = 1 (t-strides ignored, lengths null), s_init = s_final = the state; no workspace.
  */

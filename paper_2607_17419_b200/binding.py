@@ -671,6 +671,8 @@ def _rope_args(q, k, q_weight, k_weight, positions, offset, inv_freq, interleave
     for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
         if w is not None:
             _want_contiguous(name, w, q, (d,))
+    if not -2 ** 63 <= offset < 2 ** 63:
+        raise ValueError("offset must fit 64 bits")
     rotary_dim = 2 * len(inv_freq)
     freq = (ctypes.c_double * max(1, len(inv_freq)))(*inv_freq)
     a = NormRopeArgs(B=B, T=T, H_q=H, H_k=k.shape[1] if k is not None else 0, d=d, rotary_dim=rotary_dim, interleaved=int(bool(interleaved)), eps=eps,

@@ -2,8 +2,8 @@
 //   S <- a_t S + s_t k_t v_t^T,  o_t = S^T q_t + D v_t
 // One CTA per head and segment of the tokens, the state in registers: a thread has one column and a quarter of the rows.  Tokens are
 // staged 16 at a time (s_t folded into the keys), the next 16 on their way meanwhile; the four sums of an output meet in shared
-// memory.  Bound by fp32 issue: three operations per state entry and token. n = d_v = 64, fp32: 17.6 us for 128 tokens of one head alone on an SM
-// (latency), 13 us a head where an SM has several; fp32, 128 heads x 2000 tokens: 281 us.
+// memory.  Bound by fp32 issue, three operations per state entry and token, where an SM has several CTAs, and by their latency where
+// it has one.  Measured, fp32, n = d_v = 64, 128 tokens of a head: 13 and 17.6 us; 128 heads x 2000 tokens: 281 us.
 // Few heads: the token axis is cut into segments.  Their own states (from zero) come first, ssm_prefix turns them into the states
 // before the segments, and the second pass starts from those.
 #include <cmath>

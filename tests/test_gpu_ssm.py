@@ -214,3 +214,27 @@ def test_steep_and_flat_decays():
         S = init.clone()
         out = kb.kata_fwd_ssm_scan(q, k, v, dt, A, D, s_init=S, s_final=S, impl=impl)
         check(out, S, ref, "bf16", T, 64, impl == 0)
+
+
+@pytest.mark.parametrize("n", [64, 128])
+def test_step_sizes_of_either_sign(n):
+    """Without the softplus steps may be negative, and states grow in places."""
+    B, H, T = 2, 3, 200
+    q, k, v, _, _, D, _, init, gen = tensors("bf16", B, H, 1, T, n, 64, 21)
+    dt = (0.05 * torch.randn(B, H, T, device="cuda", generator=gen)).bfloat16()
+    A = torch.tensor([-2.0, 0.0, 3.0], device="cuda")
+    ref = ssm(q, k, v, dt, A, D, init=init)
+    for impl in (0, 1):
+        S = init.clone()
+        check(kb.kata_fwd_ssm_scan(q, k, v, dt, A, D, s_init=S, s_final=S, impl=impl), S, ref, "bf16", T, n, impl == 0)
+
+
+@pytest.mark.parametrize("dtype,B,H,T,n,d", [("f32", 1, 2, 512, 16, 16), ("f32", 1, 3, 3000, 64, 64), ("bf16", 1, 2, 5000, 32, 32), ("f32", 2, 2, 33, 128, 16)])
+def test_segments_token_by_token(dtype, B, H, T, n, d):
+    """Few heads: many short segments, the last one ragged, sequences that end before some of them begin."""
+    q, k, v, dt, A, D, bias, init, _ = tensors(dtype, B, H, 1, T, n, d, 23)
+    for lengths in (None, torch.tensor([T // 3, T][:B], dtype=torch.int32, device="cuda")):
+        ref = ssm(q, k, v, dt, A, D, bias, True, init, lengths)
+        S = init.clone()
+        check(kb.kata_fwd_ssm_scan(q, k, v, dt, A, D, bias, dt_softplus=True, s_init=S, s_final=S, lengths=lengths), S, ref, dtype, T, n, False)
+        check(kb.kata_fwd_ssm_scan(q, k, v, dt, A, D, bias, dt_softplus=True, s_init=init, lengths=lengths), None, ref, dtype, T, n, False)

@@ -249,3 +249,12 @@ def test_no_unbounded_wait_between_the_warps():
         for line in open(os.path.join(ROOT, "paper_2607_17419_b200", "csrc", name)):
             code = line.split("//")[0]
             assert not re.search(r"\?.*(row_sum|_sync)\s*\(", code), (name, line)
+
+
+def test_offset_of_more_than_64_bits():
+    import torch
+    q = torch.zeros(1, 1, 2, 16)
+    for offset in (1 << 63, -(1 << 63) - 1):
+        with pytest.raises(ValueError, match="offset"):
+            kb._rope_args(q, None, None, None, None, offset, (1.0,) * 8, False, 1e-6)
+    assert kb._rope_args(q, None, None, None, None, (1 << 63) - 1, (1.0,) * 8, False, 1e-6).pos_offset == (1 << 63) - 1
