@@ -434,10 +434,12 @@ tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   } else if (warp == 3) {
     // =========================== TMA loads ===========================
     if (lane == 0) {
+      int asked = 0;
       for (int j = 0; j < w.tiles && ok; ++j) {
         const int s = j % NST, tok = w.t0 + j * CT;
         ok = wait_or_abort(bars + BAR_EMPTY + s, ((j / NST) & 1) ^ 1, abort_flag);
         if (!ok) break;
+        ++asked;
         mbar_arrive_expect_tx(bars + BAR_FULL + s, Sh::STAGE);
 #pragma unroll
         for (int i = 0; i < Sh::HALVES; ++i) {
@@ -446,6 +448,7 @@ tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
         tma_load_4d(vtile(s), &tmV, bars + BAR_FULL + s, 0, tok, w.h * a.vh, w.b * a.vb);
       }
+      for (int j = max(0, asked - NST); j < asked; ++j) mbar_wait(bars + BAR_FULL + j % NST, (j / NST) & 1);     // none is in flight when the CTA ends
     }
   } else if (warp < W_WEIGHT0) {
     // =========================== state ===========================
@@ -658,7 +661,7 @@ tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if ((warp == 1 || warp == 2) && lane == 0) {
+  if ((warp == 1 || warp == 2) && elect_one()) {
     mma_commit(bars + BAR_DRAIN);
     mbar_wait(bars + BAR_DRAIN, 0);
   }
@@ -719,15 +722,18 @@ tc_ssm_state_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   if (warp == 0) {
     // =========================== TMA loads ===========================
     if (lane == 0) {
+      int asked = 0;
       for (int j = 0; j < w.tiles && ok; ++j) {
         const int s = j % NST, tok = w.t0 + j * CT;
         ok = wait_or_abort(bars + BAR_EMPTY + s, ((j / NST) & 1) ^ 1, abort_flag);
         if (!ok) break;
+        ++asked;
         mbar_arrive_expect_tx(bars + BAR_FULL + s, Sh::STAGE);
 #pragma unroll
         for (int i = 0; i < Sh::HALVES; ++i) tma_load_4d(ktile(s) + i * HALF, &tmK, bars + BAR_FULL + s, i * 64, tok, w.g * a.kg, w.b * a.kb);
         tma_load_4d(vtile(s), &tmV, bars + BAR_FULL + s, 0, tok, w.h * a.vh, w.b * a.vb);
       }
+      for (int j = max(0, asked - NST); j < asked; ++j) mbar_wait(bars + BAR_FULL + j % NST, (j / NST) & 1);     // none is in flight when the CTA ends
     }
   } else if (warp == 1) {
     // =========================== own state of the tile K^T V' ===========================
@@ -825,7 +831,7 @@ tc_ssm_state_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 1 && lane == 0) {
+  if (warp == 1 && elect_one()) {
     mma_commit(bars + BAR_DRAIN);
     mbar_wait(bars + BAR_DRAIN, 0);
   }
