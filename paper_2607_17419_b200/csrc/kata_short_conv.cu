@@ -369,8 +369,8 @@ __global__ void __launch_bounds__(kThreads) short_conv_bwd_kernel(const __grid_c
 }
 
 // ---- rows of whole 16-byte units, sequences of some length: tiles through shared memory ----
-// The walk above has a few loads of 4 bytes per thread in flight, and its time is their latency (8 x 4096 x 1024 bf16, forward and
-// gradients: 120 us).  Here a block asks for its whole tile at once by asynchronous copies of 16 bytes, which also put zeros where a
+// The walk above has a few loads of 4 bytes per thread in flight, and its time is their latency (8 x 4096 x 1024 bf16: forward 47 us,
+// with the gradients 132).  Here a block asks for its whole tile at once by asynchronous copies of 16 bytes, which also put zeros where a
 // token is not the sequence's, and several blocks share an SM; a thread then walks a run of tokens of two channels in shared memory.
 constexpr int kRun = 32, kBwdRun = 16;         // (the backward has twice two tensors of a tile in shared memory)
 
@@ -500,7 +500,9 @@ __global__ void __launch_bounds__(kThreads) short_conv_tile_kernel(const __grid_
 }
 
 // A block has one group of channels and every gridDim.y-th tile: the next tile is on its way while one is worked on, and the sums of
-// the weights stay in registers.  part: [gridDim.y][W + 1][D], or null
+// the weights stay in registers.  8 x 4096 x 1024, forward and backward: 93 us (floor 51), bound by instructions and their latency
+// (122 registers; three and four blocks on an SM: 97, 93).  Not kept: a run's last gradients from the next run through shared memory
+// instead of once more (96), the sigmoid's constants in scalar instructions (95).  part: [gridDim.y][W + 1][D], or null
 template <typename T, int W, bool SILU>
 __global__ void __launch_bounds__(kThreads, 2) short_conv_bwd_tile_kernel(const __grid_constant__ ShortConv a, int tiles, unsigned n_tiles, int shift, bool wide,
                                                                           float* __restrict__ part) {
@@ -611,7 +613,8 @@ __global__ void __launch_bounds__(kThreads, 2) short_conv_bwd_tile_kernel(const 
   }
 }
 
-// dweight[c][j] and dbias[c]: the blocks' sums added in order, eight runs of them side by side.
+// dweight[c][j] and dbias[c]: the blocks' sums added in order, eight runs of them side by side, eight loads of a run in flight (backward
+// of 16 x 31 x 1024: 11.6 us in all, one load at a time 13).
 __global__ void __launch_bounds__(256) short_conv_sum_kernel(const float* __restrict__ part, int blocks, int W, int D,
                                                              float* __restrict__ dweight, float* __restrict__ dbias) {
   __shared__ float red[8][33];
@@ -619,6 +622,7 @@ __global__ void __launch_bounds__(256) short_conv_sum_kernel(const float* __rest
   const int e = blockIdx.x * 32 + threadIdx.x, n = (W + 1) * D;
   float sum = 0.f;
   if (e < n)
+#pragma unroll 8
     for (int b = threadIdx.y; b < blocks; b += 8) sum += part[(size_t)b * n + e];
   red[threadIdx.y][threadIdx.x] = sum;
   __syncthreads();
@@ -639,8 +643,8 @@ struct ConvGrid {
   long long row_blocks;
 };
 // Segments of 32 tokens; shorter ones (down to 8, backward 16: its sums are per segment) while there are fewer threads than the GPU
-// holds.  Measured, us, bf16, segments of 8 / 16 / 32 / 64: 1 x 4096 x 1000 channels forward 6.1 / 6.7 / 8.0 / 8.8, backward 24.4 / 20.2 /
-// 25.6 / 36.3; 8 x 4096 x 1000 forward 44.5 / 41.0 / 39.2 / 46.2, backward 192 / 147 / 124 / 131.
+// holds.  Measured, us, bf16, segments of 8 / 16 / 32 / 64: 1 x 4096 x 1000 channels forward 6.1 / 6.7 / 8.0 / 8.8, backward 18.3 / 13.5 /
+// 17.6 / 27.5; 8 x 4096 x 1000 forward 44.5 / 41.0 / 39.2 / 46.2, backward 147 / 106 / 85 / 85.
 ConvGrid conv_grid(int B, int T, int D, int vec, bool backward) {
   ConvGrid g;
   g.groups = (D + vec - 1) / vec;
@@ -685,16 +689,17 @@ TileGrid tile_grid(int B, int T, int D, int elem, int run) {
   return g;
 }
 // Tiles need rows of whole 16-byte units and, so that they are worth their start and are not mostly empty, sizes of these rules.
-// Measured, us, walk / tiles, T x 1024 channels of 32768 tokens unless others are named:
+// Measured, us, walk / tiles, 1024 channels, 32768 tokens unless others are named:
 //   forward, bf16: T = 64: 47 / 49, 128: 48 / 27, 16384: 47 / 27; 4096 tokens: 6.8 / 6.3, 1024 tokens: 3.8 / 4.4
 //   forward, fp32: T = 64: 66 / 90, 128: 66 / 48; 8192 tokens: 17.5 / 16.4, 4096 tokens: 9.4 / 10.8
-//   backward, bf16, 16384 tokens: T = 32: 72 / 95, 64: 72 / 62, 128: 72 / 52; 8192 tokens (two rounds of tiles begun): 41 / 32, 4096 (two, the
-//   second nearly empty): 20 / 24, 2048 (one): 15.8 / 15.2.  Backward in fp32: 104 / 110, 189 / 209 of 32768 tokens: never.
+//   backward, bf16, sequences x T: 512 x 32: 46 / 46, 128 x 32: 14 / 17, 512 x 48: 77 / 68, 256 x 64: 47 / 38, 8 x 4096: 82 / 69; in rounds of
+//   tiles: 64 x 128 (more than two) 26 / 22, 32 x 128 (the second nearly empty) 14.3 / 14.4, 16 x 128 (one) 11.9 / 8.9
+//   backward, fp32: 16384 tokens 69 / 82, 32768: 122 / 161: never tiles
 bool use_tiles(const ShortConv& a, bool backward) {
   const int e = a.dtype == KATA_F32 ? 4 : 2;
   if ((a.D * e) % 16 != 0 || !conv_aligned(a, a.x, 16)) return false;
   if (!backward) return a.T >= 128 && (double)a.B * a.T * a.D >= (e == 2 ? 1 << 21 : 1 << 23);
-  if (e != 2 || a.T < 64 || !conv_aligned(a, a.dout, 16)) return false;
+  if (e != 2 || a.T < 48 || !conv_aligned(a, a.dout, 16)) return false;
   const TileGrid g = tile_grid(a.B, a.T, a.D, e, kBwdRun);
   return g.n_tiles <= g.walkers || g.n_tiles >= 2 * g.walkers;
 }
