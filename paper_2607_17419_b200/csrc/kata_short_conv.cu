@@ -613,8 +613,8 @@ __global__ void __launch_bounds__(kThreads, 2) short_conv_bwd_tile_kernel(const 
   }
 }
 
-// dweight[c][j] and dbias[c]: the blocks' sums added in order, eight runs of them side by side, eight loads of a run in flight (backward
-// of 16 x 31 x 1024: 11.6 us in all, one load at a time 13).
+// dweight[c][j] and dbias[c]: the blocks' sums added in order, eight runs of them side by side, eight loads of a run in flight (forward
+// and backward of 16 x 31 x 1024: 11.3 us, one load at a time 13.0).
 __global__ void __launch_bounds__(256) short_conv_sum_kernel(const float* __restrict__ part, int blocks, int W, int D,
                                                              float* __restrict__ dweight, float* __restrict__ dbias) {
   __shared__ float red[8][33];
@@ -694,7 +694,7 @@ TileGrid tile_grid(int B, int T, int D, int elem, int run) {
 //   forward, fp32: T = 64: 66 / 90, 128: 66 / 48; 8192 tokens: 17.5 / 16.4, 4096 tokens: 9.4 / 10.8
 //   backward, bf16, sequences x T: 512 x 32: 46 / 46, 128 x 32: 14 / 17, 512 x 48: 77 / 68, 256 x 64: 47 / 38, 8 x 4096: 82 / 69; in rounds of
 //   tiles: 64 x 128 (more than two) 26 / 22, 32 x 128 (the second nearly empty) 14.3 / 14.4, 16 x 128 (one) 11.9 / 8.9
-//   backward, fp32: 16384 tokens 69 / 82, 32768: 122 / 161: never tiles
+//   backward, fp32 (with the forward, less the forward): 16384 tokens 69 / 82, 32768: 122 / 161: never tiles
 bool use_tiles(const ShortConv& a, bool backward) {
   const int e = a.dtype == KATA_F32 ? 4 : 2;
   if ((a.D * e) % 16 != 0 || !conv_aligned(a, a.x, 16)) return false;
