@@ -55,10 +55,10 @@ __global__ void __launch_bounds__(DEC_THREADS) decode_update_kernel(const T* __r
   const int bh = blockIdx.y, slab = blockIdx.x, n_slabs = gridDim.x;
   const int tid = threadIdx.x;
   // Launched with programmatic stream serialisation: the CTAs may be resident before the kernel ahead in the stream
-  // (the producer of q, k, v, or the previous step's finish kernel, which still reads `part`) has ended, and let the kernel
-  // behind become resident at once.
-  cudaTriggerProgrammaticLaunchCompletion();
+  // (the producer of q, k, v, or the previous step's finish kernel, which still reads `part`) has ended.  The finish kernel
+  // reads q and k ahead of its own wait, so it may become resident only when their producer has ended: behind this wait.
   cudaGridDependencySynchronize();
+  cudaTriggerProgrammaticLaunchCompletion();
   // k_hat = k / ||k|| (zero row -> zero feature); the query norm cancels in the readout and is not applied
   if (tid < 64) {
     float kv = tid < d_k ? to_f32<T>(k[(size_t)bh * d_k + tid]) : 0.f;
@@ -174,7 +174,8 @@ __global__ void decode_finish_kernel(const float* __restrict__ part, const T* __
   }
   if (order != 1) w *= inv_or_zero(kk);     // raw q: the query norm cancels in the ratio
   // Launched with programmatic stream serialisation: everything above ran while the update kernel was still
-  // streaming the state; its partial sums are visible from here on.
+  // streaming the state (which lets this kernel start only when what is ahead of both has ended); its partial sums are
+  // visible from here on.
   cudaGridDependencySynchronize();
   if (c >= DV) return;
   float num = 0.f, den = 0.f;

@@ -88,7 +88,9 @@ __device__ __forceinline__ float2 add_pair(float2 a, float2 b) {
 }
 
 // Launches with programmatic stream serialisation: the kernel may become resident before the one ahead of it in the stream has
-// ended, and waits for it (cudaGridDependencySynchronize) before it touches memory.
+// ended, and waits for it (cudaGridDependencySynchronize) before it touches memory.  It lets the kernel behind become resident
+// before it has waited itself, so a kernel that is launched behind it in this way must not touch memory ahead of its wait either;
+// one that has to (the decode step's second kernel) stands behind a kernel that waits first and lets it start then.
 // early = false: it starts when that kernel has ended.
 template <typename... P, typename... A>
 inline void launch_when(bool early, LaunchCtx& ctx, void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, A&&... args) {
