@@ -10,7 +10,8 @@
 // its own, from V scaled and rounded to bf16) and leave a bf16 copy in shared memory for the next tile's Q S.
 // The weights of a 32 x 32 block are a row factor times a column factor, taken at the start of the rows' block: below the diagonal
 // both are at most s_i; on the diagonal they are taken at half of the block's decay, and only blocks that decay by more than 2^-240 in
-// their 32 tokens take an exponential per entry instead.  So a tile takes a few exponentials per token and two products per score.
+// their 32 tokens, or whose step sizes take such a factor out of fp32's range, take an exponential per entry instead.  So a tile takes
+// a few exponentials per token and two products per score.
 // tc_ssm_state_kernel: the segments' own states (several segments, or a final state wanted).  For a final state they are exact to
 // fp32: the scaled V goes in as three bf16 terms (24 bits), the small ones first; every tile's product is added in registers.
 //
@@ -54,9 +55,8 @@ struct Decays {
   float before[4];                               // 2^(c from the start of the tile to block b)
   float between[4][4];                           // [r][b]: 2^(c from the end of block b to the start of block r), b < r
   float total;                                   // 2^(c of the whole tile)
-  int steep;                                     // bit b: block b decays (or grows) by more than 2^240
   float half[4];                                 // m
-  float pad[2];
+  float pad[3];
 };
 
 template <int N, int STATE> struct Shape {         // STATE: terms of the scaled V in the state kernel; 0: the out kernel
@@ -248,7 +248,6 @@ __device__ __forceinline__ double decay_warp(int first, const Args& a, const Whe
       reinterpret_cast<float4*>(d.inv)[lane] = make_float4(s[0] * ex2(m - c[0]), s[1] * ex2(m - c[1]), s[2] * ex2(m - c[2]), s[3] * ex2(m - c[3]));
       reinterpret_cast<float4*>(d.rel)[lane] = make_float4(c[0], c[1], c[2], c[3]);
       reinterpret_cast<float4*>(d.step)[lane] = make_float4(s[0], s[1], s[2], s[3]);
-      const unsigned steep = __ballot_sync(0xffffffffu, !(fabsf(c[0] - m) < 120.f && fabsf(c[1] - m) < 120.f && fabsf(c[2] - m) < 120.f && fabsf(c[3] - m) < 120.f));
       if ((lane & 7) == 0) d.half[blk] = m;
       // lanes 0-3: before; 4: the whole tile; 5: [2][0], 6: [3][0], 7: [3][1]; neighbours are 1
       const float e = ex2(lane == 1 ? b0 : lane == 2 ? b0 + b1 : lane == 3 ? b0 + b1 + b2 : lane == 4 ? (b0 + b1) + (b2 + b3) : lane == 5 ? b1
@@ -257,7 +256,6 @@ __device__ __forceinline__ double decay_warp(int first, const Args& a, const Whe
       if (lane == 4) d.total = e;
       if (lane >= 5 && lane < 8) d.between[lane == 5 ? 2 : 3][lane == 7 ? 1 : 0] = e;
       if (lane >= 8 && lane < 11) d.between[lane - 7][lane - 8] = 1.f;
-      if (lane == 11) d.steep = ((steep & 0xffu) != 0 ? 1 : 0) | ((steep & 0xff00u) != 0 ? 2 : 0) | ((steep & 0xff0000u) != 0 ? 4 : 0) | ((steep >> 24) != 0 ? 8 : 0);
     } else if (lane == 0) {
       d.total = ex2((b0 + b1) + (b2 + b3));
     }
@@ -544,8 +542,17 @@ tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           const float4* col = reinterpret_cast<const float4*>((diag ? d.inv : d.tail) + blk * 32);
           const float f = diag ? ex2(rel - d.half[blk]) : rf * d.between[q4][blk];
           const float2 ff = make_float2(f, f);
+          // A block is steep where a factor leaves fp32's normal range, the step size with it: 1000 2^119 would be inf, 2^-20 2^-118
+          // has lost bits or is zero, and so would be their product with the row's factor, which is s_i itself on the diagonal.
+          // Every lane looks at its own token.  (Here and not where the factors are formed: that warp's instructions count, and the
+          // test there took 8 x 16 heads x 4096 tokens from 59.3 us to 62.9.)
+          bool steep = false;
+          if (diag) {
+            const float inv = fabsf(d.inv[row]);
+            steep = __any_sync(0xffffffffu, !(fabsf(rel - d.half[blk]) < 120.f && (d.step[row] == 0.f || (inv >= 0x1p-126f && inv < 0x1p126f))));
+          }
           tmem_wait_ld(y);
-          if (diag && ((d.steep >> blk) & 1)) {
+          if (steep) {
 #pragma unroll
             for (int c = 0; c < 32; c += 2)
               pk[c / 2] = pack_bf16(__uint_as_float(y[c]) * (d.step[blk * 32 + c] * ex2(rel - d.rel[blk * 32 + c])),

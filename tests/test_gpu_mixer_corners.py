@@ -1,0 +1,44 @@
+"""Scan and short convolution where their arithmetic has corners: step sizes far from one another, entries that are not finite."""
+import pytest
+import torch
+
+from paper_2607_17419_b200 import binding as kb
+
+from mixer_ref import F32, live_mask, ssm
+from test_gpu_ssm import check, tensors
+
+pytestmark = pytest.mark.gpu
+
+
+def both_forms(dt, A, n, seed, T):
+    """Tensor cores and token by token against the recurrence, with and without a state."""
+    B, H = dt.shape[:2]
+    q, k, v, _, _, D, _, init, _ = tensors("bf16", B, H, 1, T, n, 64, seed)
+    for first in (None, init):
+        ref = ssm(q, k, v, dt, A, init=first)
+        for impl in (kb.KATA_IMPL_TENSOR, kb.KATA_IMPL_SIMT):
+            S = torch.empty_like(init)
+            out = kb.kata_fwd_ssm_scan(q, k, v, dt, A, s_init=first, s_final=S, impl=impl)
+            check(out, S, ref, "bf16", T, n, impl == kb.KATA_IMPL_TENSOR)
+
+
+@pytest.mark.parametrize("n", [64, 128])
+@pytest.mark.parametrize("at", [0, 7, 30, 31])
+def test_one_large_step_of_a_slow_head(n, at):
+    """The decay of a block is of ordinary size, the step alone is large: products of factors must not leave fp32."""
+    H, T = 8, 200
+    dt = torch.full((1, H, T), 0.01, device="cuda").bfloat16()
+    dt[:, :, at::96] = 1000.0
+    A = torch.tensor([-0.05, -0.08, -0.11, -0.14, -0.16, -0.165, -0.168, -0.17], device="cuda")
+    both_forms(dt, A, n, 31, T)
+
+
+@pytest.mark.parametrize("size", [2.0 ** -20, 2.0 ** -40, 2.0 ** -60])
+def test_small_steps_before_a_strong_decay(size):
+    """Steps of next to nothing in a block that decays by up to 2^230: their own outputs are as exact as others."""
+    H, T = 4, 200
+    dt = torch.full((2, H, T), size, device="cuda").bfloat16()
+    dt[0, :, 20::64] = 1.0
+    dt[1, :, 3::32] = 1.0
+    A = torch.tensor([-60.0, -100.0, -130.0, -158.0], device="cuda")
+    both_forms(dt, A, 64, 33, T)
