@@ -209,7 +209,10 @@ __device__ __forceinline__ double decay_warp(int first, const Args& a, const Whe
       const float o = __shfl_up_sync(0xffffffffu, upto, off, 8);
       if ((lane & 7) >= off) upto += o;
     }
-    const float base = upto - sum, mine = __shfl_sync(0xffffffffu, upto, 7, 8);     // before this lane's tokens; of the whole block
+    // before this lane's tokens (their own sum taken off `upto` again would leave its rounding, 2^-3 where they lose 2^21); of the whole block
+    float base = __shfl_up_sync(0xffffffffu, upto, 1, 8);
+    if ((lane & 7) == 0) base = 0.f;
+    const float mine = __shfl_sync(0xffffffffu, upto, 7, 8);
     // What a token loses up to the end of its block, summed from the end: as a difference it would carry the rounding of the whole
     // block's sum, 2^-19 of the weight where the block decays by 2^-50.
     float after = 0.f, lost[4];
@@ -553,10 +556,18 @@ tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           }
           tmem_wait_ld(y);
           if (steep) {
+            // Column by column from the diagonal backwards, what a token loses to the row summed on the way: as a difference of sums
+            // from the block's start it would carry the rounding of a token that forgets everything (18 % where that loses 2^21).
+            const float rate = a.A[w.h] * 1.44269504f;
+            float lost = 0.f;
 #pragma unroll
-            for (int c = 0; c < 32; c += 2)
-              pk[c / 2] = pack_bf16(__uint_as_float(y[c]) * (d.step[blk * 32 + c] * ex2(rel - d.rel[blk * 32 + c])),
-                                    __uint_as_float(y[c + 1]) * (d.step[blk * 32 + c + 1] * ex2(rel - d.rel[blk * 32 + c + 1])));
+            for (int c = 30; c >= 0; c -= 2) {
+              const float s1 = d.step[blk * 32 + c + 1], s0 = d.step[blk * 32 + c], w1 = s1 * ex2(lost);
+              if (c + 1 <= lane) lost = fmaf(s1, rate, lost);
+              const float w0 = s0 * ex2(lost);
+              if (c <= lane) lost = fmaf(s0, rate, lost);
+              pk[c / 2] = pack_bf16(__uint_as_float(y[c]) * w0, __uint_as_float(y[c + 1]) * w1);
+            }
           } else {
 #pragma unroll
             for (int c = 0; c < 32; c += 4) {

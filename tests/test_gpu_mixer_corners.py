@@ -42,3 +42,15 @@ def test_small_steps_before_a_strong_decay(size):
     dt[1, :, 3::32] = 1.0
     A = torch.tensor([-60.0, -100.0, -130.0, -158.0], device="cuda")
     both_forms(dt, A, 64, 33, T)
+
+
+@pytest.mark.parametrize("large,small,rate", [(1e5, 0.01, -16.0), (1000.0, 1e-4, -1000.0), (3e4, 0.05, -8.0), (40.0, 0.02, -11.0)])
+def test_small_steps_around_one_that_forgets(large, small, rate):
+    """A step that forgets everything, anywhere in a block, with ordinary ones before and behind it: what they lose to one another
+    must not drown in what that step loses."""
+    places = [0, 1, 2, 3, 5, 10, 15, 30, 31]
+    T = 200
+    dt = torch.full((len(places), 2, T), small, device="cuda").bfloat16()
+    for b, at in enumerate(places):
+        dt[b, :, at::96] = large
+    both_forms(dt, torch.tensor([rate, 0.5 * rate], device="cuda"), 64, 35, T)
