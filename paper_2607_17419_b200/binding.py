@@ -638,6 +638,8 @@ def _frequencies(base: float, rotary_dim: int):
 
 def _rope_freq(q, base, inv_freq, rotary_dim):
     """The angles per position, a tuple or list of floats."""
+    if rotary_dim is not None and (rotary_dim < 0 or rotary_dim % 2 != 0):
+        raise ValueError(f"rotary_dim is {rotary_dim}: entries are turned in pairs")
     if inv_freq is None:
         if rotary_dim is None:
             rotary_dim = q.shape[-1] if isinstance(q, torch.Tensor) and q.dim() > 0 else 0
