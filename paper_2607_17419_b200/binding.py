@@ -586,6 +586,8 @@ def _want(name: str, t, q, shape, dtype=None):
         raise ValueError(f"{name} must be a tensor")
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} is {tuple(t.shape)}, the call needs {tuple(shape)}")
+    if any(n > 0x7fffffff for n in shape):               # (the argument structs have 32 bits, ctypes would keep the low ones)
+        raise ValueError(f"{name} is {tuple(t.shape)}: the library counts in 32 bits")
     dtype = q.dtype if dtype is None else dtype
     if t.dtype is not dtype:
         raise ValueError(f"{name} is {t.dtype}, the call needs {dtype}")
