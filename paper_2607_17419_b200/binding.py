@@ -879,6 +879,8 @@ def kata_fwd_ssm_scan(q, k, v, dt, A, D=None, dt_bias=None, *, dt_softplus: bool
         r = _native_result("kata_fwd_ssm_scan", (_native or native()).ssm(_default_scratch, q, k, v, dt, A, D, dt_bias, dt_softplus, s_init, s_final, lengths, out, impl))
         if r is not NotImplemented:
             return r
+    if not -0x80000000 <= impl <= 0x7fffffff:
+        raise ValueError("impl must fit 32 bits")
     a, out = _ssm_args(q, k, v, dt, A, D, dt_bias, dt_softplus, lengths, out)
     for name, s in (("s_init", s_init), ("s_final", s_final)):
         if s is not None:

@@ -289,6 +289,13 @@ PyObject* backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // ---- rows around the attention and the decayed recurrence (binding.py: the functions of the same names) ----
 // Strided views whose rows lie side by side, on the current device; everything else is left to binding.py.
 
+// The truth of an option; false: it has none (binding.py raises what asking for it raises).
+bool truth(PyObject* o, int32_t& to) {
+  const int x = PyObject_IsTrue(o);
+  if (x < 0) PyErr_Clear();
+  to = x == 1;
+  return x >= 0;
+}
 // The tensor if it is plain, has these sizes and this type, and lies on main's device (main: itself).
 const at::Tensor* view(PyObject* o, const at::Tensor* main, std::initializer_list<int64_t> sizes, at::ScalarType type, bool contiguous = false) {
   const at::Tensor* t = plain(o);
@@ -383,7 +390,7 @@ bool rope_args(PyObject* const* a, kata_norm_rope_args& r, double (&freq)[64], k
   }
   r.inv_freq = freq;
   r.rotary_dim = (int)(2 * n);
-  r.interleaved = PyObject_IsTrue(a[7]) == 1;
+  if (!truth(a[7], r.interleaved)) return false;
   r.eps = PyFloat_AS_DOUBLE(a[8]);
   r.q = q->data_ptr();
   strides(*q, r.q_stride, 3);
@@ -473,7 +480,7 @@ bool conv_args(PyObject* const* a, int64_t dim, kata_short_conv_args& r, kata_op
   r.width = (int)w->size(1);
   r.weight = w->data_ptr();
   if (!optional(a[2], *x, {r.D}, x->scalar_type(), r.bias) || !optional(a[4], *x, {r.B}, at::kInt, r.lengths)) return false;
-  r.silu = PyObject_IsTrue(a[3]) == 1;
+  if (!truth(a[3], r.silu)) return false;
   r.x = x->data_ptr();
   strides(*x, r.x_stride, (int)dim - 1);
   return true;
@@ -554,9 +561,9 @@ PyObject* ssm(PyObject*, PyObject* const* a, Py_ssize_t n) {
       !optional(a[7], *v, {r.H}, at::kFloat, r.dt_bias) || !optional(a[9], *v, {r.B, r.H, r.n, r.d_v}, at::kFloat, r.s_init) ||
       !optional(a[10], *v, {r.B, r.H, r.n, r.d_v}, at::kFloat, r.s_final) || !optional(a[11], *v, {r.B}, at::kInt, r.lengths) || !given_fits(a[12], *v))
     return not_implemented();
-  r.dt_softplus = PyObject_IsTrue(a[8]) == 1;
-  const long impl = PyLong_AsLong(a[13]);
-  if (impl < INT_MIN || impl > INT_MAX) return not_implemented();
+  int overflow = 0;
+  const long impl = PyLong_AsLongAndOverflow(a[13], &overflow);
+  if (!truth(a[8], r.dt_softplus) || overflow != 0 || impl < INT_MIN || impl > INT_MAX) return not_implemented();
   o.impl = (int)impl;
   PyObject* held = nullptr;
   if (step) o.stream = c10::cuda::getCurrentCUDAStream(v->device().index()).stream();

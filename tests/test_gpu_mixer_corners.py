@@ -54,3 +54,17 @@ def test_small_steps_around_one_that_forgets(large, small, rate):
     for b, at in enumerate(places):
         dt[b, :, at::96] = large
     both_forms(dt, torch.tensor([rate, 0.5 * rate], device="cuda"), 64, 35, T)
+
+
+def test_options_without_a_truth_or_too_large():
+    """An option that has no truth, or no 32 bits, raises what it raises through ctypes, and nothing is left pending."""
+    two = torch.tensor([True, False])
+    x, w, q = (torch.zeros(*s, device="cuda", dtype=torch.bfloat16) for s in ((2, 5, 64), (64, 4), (1, 2, 5, 64)))
+    dt, A = torch.zeros(1, 2, 5, device="cuda", dtype=torch.bfloat16), torch.zeros(2, device="cuda")
+    for call in (lambda: kb.kata_fwd_short_conv(x, w, silu=two), lambda: kb.kata_bwd_short_conv(x, x, w, silu=two), lambda: kb.kata_fwd_norm_rope(q, interleaved=two),
+                 lambda: kb.kata_fwd_ssm_scan(q, q, q, dt, A, dt_softplus=two)):
+        with pytest.raises(RuntimeError, match="ambiguous"):
+            call()
+    for impl in (1 << 70, -(1 << 70), 1 << 32):
+        with pytest.raises(ValueError, match="impl"):
+            kb.kata_fwd_ssm_scan(q, q, q, dt, A, impl=impl)
