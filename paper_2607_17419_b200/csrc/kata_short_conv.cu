@@ -533,8 +533,8 @@ __global__ void __launch_bounds__(kThreads, 2) short_conv_bwd_tile_kernel(const 
     wait_copies<1>();
     __syncthreads();
     const Tile p = tile_at(index, tiles, tile_tokens, blockIdx.x);
-    const int t0 = p.t0 + threadIdx.y * kBwdRun;
-    if (on && t0 < a.T) {
+    const int t0 = p.t0 + threadIdx.y * kBwdRun, len = sequence_length(a.lengths, p.b, a.T);
+    if (on && t0 < len) {
       const T* xr = reinterpret_cast<const T*>(smem + k * buffer) + (size_t)threadIdx.y * kBwdRun * width + threadIdx.x * 2;
       const T* gr = reinterpret_cast<const T*>(smem + k * buffer + g_at) + (size_t)threadIdx.y * kBwdRun * width + threadIdx.x * 2;
       auto get = [&](const T* rows, int row) {
@@ -594,6 +594,14 @@ __global__ void __launch_bounds__(kThreads, 2) short_conv_bwd_tile_kernel(const 
       for (int u = W - 1; u < kBwdRun; ++u) token(u, true, true);
 #pragma unroll
       for (int u = kBwdRun; u < kBwdRun + W - 1; ++u) token(u, false, true);
+    }
+    // Rows behind the end.  (The last run has stored some: zeros, but NaN where an input before the end is not finite.)
+    if (on && a.lengths != nullptr) {
+      T* to = reinterpret_cast<T*>(a.dx.p) + (long long)p.b * a.dx.s0 + c;
+      Entries<T, 2> e;
+      e.zero();
+#pragma unroll 1
+      for (int t = max(t0, len); t < min(t0 + kBwdRun, a.T); ++t) e.store(to + (long long)t * a.dx.s1);
     }
     __syncthreads();                                             // the buffer may be asked into again
   }

@@ -68,3 +68,39 @@ def test_options_without_a_truth_or_too_large():
     for impl in (1 << 70, -(1 << 70), 1 << 32):
         with pytest.raises(ValueError, match="impl"):
             kb.kata_fwd_ssm_scan(q, q, q, dt, A, impl=impl)
+
+
+def conv_case(T, lengths, silu, seed=5):
+    """bf16 rows of whole units, 48 tokens or more: gradients through tiles; the same rows one entry further on: token by token."""
+    B, D, W = 4, 1024, 4
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    n = lambda *s: torch.randn(*s, device="cuda", generator=gen).bfloat16()
+    x, w, b, g = n(B, T, D), n(D, W), n(D), n(B, T, D)
+    room = torch.empty(B, T, D + 8, device="cuda", dtype=torch.bfloat16)
+    return B, D, W, x, w, b, g, room[..., 1:1 + D]
+
+
+def same(a, b):
+    return torch.equal(a.isnan(), b.isnan()) and torch.equal(a.nan_to_num(0.0), b.nan_to_num(0.0))
+
+
+@pytest.mark.parametrize("T", [48, 64, 150])
+@pytest.mark.parametrize("silu", [False, True])
+@pytest.mark.parametrize("what", [float("inf"), float("nan")])
+def test_rows_behind_the_end_are_zeros(T, silu, what):
+    """The last live inputs are not finite: what they make of a gradient stays in front of the end, whichever way rows are read."""
+    lengths = torch.tensor([T, T - 2, 17, 1], dtype=torch.int32, device="cuda")
+    B, D, W, x, w, b, g, shifted = conv_case(T, lengths, silu)
+    for s, L in enumerate(lengths.tolist()):
+        x[s, max(0, L - 2):L, 3::64] = what
+    shifted.copy_(x)
+    live = live_mask(lengths, B, T, "cuda")[..., None]
+    tile = kb.kata_bwd_short_conv(g, x, w, b, silu=silu, lengths=lengths)
+    walk = kb.kata_bwd_short_conv(g, shifted, w, b, silu=silu, lengths=lengths)
+    for dx, _, _ in (tile, walk):
+        assert torch.all(dx.masked_select(~live.expand_as(dx)) == 0)
+    assert same(tile[0], walk[0])
+    clean = torch.ones(D, dtype=torch.bool, device="cuda")
+    clean[3::64] = False
+    for _, dw, db in (tile, walk):
+        assert torch.isfinite(dw[clean]).all() and torch.isfinite(db[clean]).all()
