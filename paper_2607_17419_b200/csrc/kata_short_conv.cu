@@ -345,7 +345,7 @@ __global__ void __launch_bounds__(kThreads) short_conv_bwd_kernel(const __grid_c
         g.load(pg);
       }
       const int at = t - (W - 1);
-      emit(widen<T, VEC>(e), widen<T, VEC>(g), t < t1, at >= t0 && at < t1, at >= len, po);
+      emit(widen<T, VEC>(e), widen<T, VEC>(g), t < live, at >= t0 && at < t1, at >= len, po);
     }
   }
   if (part == nullptr) return;
@@ -542,6 +542,7 @@ __global__ void __launch_bounds__(kThreads, 2) short_conv_bwd_tile_kernel(const 
         e.load(rows + (size_t)row * width);
         return widen<T, 2>(e);
       };
+      const int left = len - t0;                                 // tokens of the sequence: no others count in the sums (0 times inf is NaN)
       Pairs<2> win[W - 1], gw[W - 1];
 #pragma unroll
       for (int j = 0; j < W - 1; ++j) {
@@ -563,7 +564,7 @@ __global__ void __launch_bounds__(kThreads, 2) short_conv_bwd_tile_kernel(const 
           const float2 sig = sigmoid_pair<T>(z.p[0]), rest = fma_pair(sig, make_float2(-1.f, -1.f), make_float2(1.f, 1.f));
           g.p[0] = mul_pair(g.p[0], fma_pair(mul_pair(z.p[0], sig), rest, sig));
         }
-        if (own) {
+        if (own && u < left) {
 #pragma unroll
           for (int j = 0; j < W - 1; ++j) dw[j].add_product(g, win[j]);
           dw[W - 1].add_product(g, now);

@@ -104,3 +104,32 @@ def test_rows_behind_the_end_are_zeros(T, silu, what):
     clean[3::64] = False
     for _, dw, db in (tile, walk):
         assert torch.isfinite(dw[clean]).all() and torch.isfinite(db[clean]).all()
+
+
+@pytest.mark.parametrize("T", [48, 64, 150])
+@pytest.mark.parametrize("padded", [False, True])
+def test_sums_take_the_tokens_of_the_sequences_alone(T, padded):
+    """Without an activation an infinite last input meets one tap alone; the sums of the others have no term behind the end."""
+    lengths = torch.tensor([T, T - 2, 17, 5], dtype=torch.int32, device="cuda") if padded else None
+    B, D, W, x, w, b, g, shifted = conv_case(T, lengths, False)
+    ends = lengths.tolist() if padded else [T] * B
+    x64 = x.double()
+    for s, L in enumerate(ends):
+        x[s, L - 1, 3::64] = float("inf")
+        g[s, L - 1, 3::64] = 1.0
+    shifted.copy_(x)
+    live = live_mask(lengths, B, T, "cuda")[..., None]
+    g64 = g.double().masked_fill(~live, 0)
+    for s, L in enumerate(ends):
+        x64[s, L - 1, 3::64] = 0                                  # (its only term is that of the last tap)
+    line = torch.cat([x64.new_zeros(B, W - 1, D), x64.masked_fill(~live, 0)], 1)
+    ref = torch.stack([(line[:, j:j + T] * g64).sum((0, 1)) for j in range(W)], 1)
+    size = torch.stack([(line[:, j:j + T] * g64).abs().sum((0, 1)) for j in range(W)], 1)
+    for rows in (x, shifted):
+        _, dw, db = kb.kata_bwd_short_conv(g, rows, w, b, silu=False, lengths=lengths)
+        assert torch.all(dw[3::64, W - 1] == float("inf"))
+        ok = torch.ones_like(dw, dtype=torch.bool)
+        ok[3::64, W - 1] = False
+        assert torch.isfinite(dw[ok]).all() and torch.isfinite(db).all()
+        # (4 T terms in a row at most, each product and sum rounded once)
+        assert torch.all(((dw - ref).abs() <= (B * T + 20) * F32 * size + 1e-38)[ok])
