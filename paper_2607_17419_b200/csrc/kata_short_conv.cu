@@ -697,20 +697,29 @@ TileGrid tile_grid(int B, int T, int D, int elem, int run) {
   if (g.walkers > 65535) g.walkers = 65535;
   return g;
 }
-// Tiles need rows of whole 16-byte units and, so that they are worth their start and are not mostly empty, sizes of these rules.
+// Tiles need rows of whole 16-byte units, a size that is worth their start, and sequences that fill them: a tile has 128 tokens (backward
+// 64) of 128 channels or more, twice as many of half as many, and so on.
 // Measured, us, walk / tiles, 1024 channels, 32768 tokens unless others are named:
 //   forward, bf16: T = 64: 47 / 49, 128: 48 / 27, 16384: 47 / 27; 4096 tokens: 6.8 / 6.3, 1024 tokens: 3.8 / 4.4
 //   forward, fp32: T = 64: 66 / 90, 128: 66 / 48; 8192 tokens: 17.5 / 16.4, 4096 tokens: 9.4 / 10.8
-//   backward, bf16, sequences x T: 512 x 32: 46 / 46, 128 x 32: 14 / 17, 512 x 48: 77 / 68, 256 x 64: 47 / 38, 8 x 4096: 82 / 69; in rounds of
-//   tiles: 64 x 128 (more than two) 26 / 22, 32 x 128 (the second nearly empty) 14.3 / 14.4, 16 x 128 (one) 11.9 / 8.9
-//   backward, fp32 (with the forward, less the forward): 16384 tokens 69 / 82, 32768: 122 / 161: never tiles
+//   backward, bf16, sequences x T: 512 x 32: 46 / 46, 128 x 32: 14 / 17, 512 x 48: 77 / 70, 256 x 64: 47 / 38, 8 x 4096: 82 / 71; in rounds of
+//   tiles: 64 x 128 (more than two) 26 / 22, 32 x 128 (the second nearly empty) 14.3 / 14.4, 16 x 128 (one) 11.9 / 9.0
+//   backward, fp32 (with the forward, less the forward): 16384 tokens 69 / 82, 32768: 120 / 161: never tiles
+// Fewer channels, 2^24 entries, and how full the tiles are (channels x T):
+//   forward, bf16: full 16 x 1024 16.6 / 13.4, 64 x 256 19.4 / 13.4, three quarters 16 x 768 16.7 / 19.0, 64 x 192 17.4 / 19.0, 1024 x 192 18.2 /
+//   19.0, half 64 x 128 19.3 / 26.0, an eighth 16 x 128 17.5 / 100; eight channels 8 x 2048 (full) 22.1 / 20.9, 8 x 128 22.6 / 220
+//   forward, fp32: full 16 x 512 37.6 / 28.8, three quarters 16 x 384 37.8 / 35.0, 64 x 192 34.1 / 34.5, half 16 x 256 38.0 / 47.6, 64 x 64 34.4 / 47.6
+//   backward, bf16: full 16 x 512 44 / 35, half 16 x 256 44 / 42, 32 x 128 50 / 42, 64 x 64 49 / 42, 3/8 16 x 192 44 / 51, an eighth 16 x 64 44 / 119;
+//   eight channels, full 8 x 1024 44 / 48, 8 x 64 44 / 229
 bool use_tiles(const ShortConv& a, bool backward) {
   const int e = a.dtype == KATA_F32 ? 4 : 2;
-  if ((a.D * e) % 16 != 0 || !conv_aligned(a, a.x, 16)) return false;
-  if (!backward) return a.T >= 128 && (double)a.B * a.T * a.D >= (e == 2 ? 1 << 21 : 1 << 23);
-  if (e != 2 || a.T < 48 || !conv_aligned(a, a.dout, 16)) return false;
-  const TileGrid g = tile_grid(a.B, a.T, a.D, e, kBwdRun);
-  return g.n_tiles <= g.walkers || g.n_tiles >= 2 * g.walkers;
+  if ((a.D * e) % 16 != 0 || a.D < 16 || !conv_aligned(a, a.x, 16)) return false;
+  if (backward && (e != 2 || !conv_aligned(a, a.dout, 16))) return false;
+  const int run = backward ? kBwdRun : kRun;
+  const TileGrid g = tile_grid(a.B, a.T, a.D, e, run);
+  const double full = (double)a.T / ((double)g.tiles * g.ty * run);
+  if (!backward) return a.T >= 128 && full >= (e == 2 ? 0.8 : 0.7) && (double)a.B * a.T * a.D >= (e == 2 ? 1 << 21 : 1 << 23);
+  return a.T >= 48 && full >= 0.5 && (g.n_tiles <= g.walkers || g.n_tiles >= 2 * g.walkers);
 }
 
 template <typename T, int W, bool SILU> void launch_tiles(const ShortConv& a, LaunchCtx& ctx) {

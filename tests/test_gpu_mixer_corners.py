@@ -4,7 +4,8 @@ import torch
 
 from paper_2607_17419_b200 import binding as kb
 
-from mixer_ref import F32, live_mask, ssm
+from mixer_ref import F32, conv, conv_bound, live_mask, ssm, within
+from test_gpu_short_conv import ragged as conv_ragged, tensors as conv_tensors, test_backward as conv_backward
 from test_gpu_ssm import check, tensors
 
 pytestmark = pytest.mark.gpu
@@ -133,3 +134,53 @@ def test_sums_take_the_tokens_of_the_sequences_alone(T, padded):
         assert torch.isfinite(dw[ok]).all() and torch.isfinite(db).all()
         # (4 T terms in a row at most, each product and sum rounded once)
         assert torch.all(((dw - ref).abs() <= (B * T + 20) * F32 * size + 1e-38)[ok])
+
+
+FILLS = [  # channels from few to many, with sequences that fill tiles of shared memory and sequences that do not: B, T, D, W
+    (150, 1024, 16, 4), (1100, 128, 16, 4), (40, 512, 64, 2), (300, 130, 32, 3), (3000, 100, 8, 2), (130, 2048, 8, 4), (24, 900, 128, 2), (600, 64, 64, 3),
+]
+
+
+@pytest.mark.parametrize("B,T,D,W", FILLS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_convolution_of_few_and_many_channels(dtype, B, T, D, W):
+    """Forward and backward whatever way rows are read; a shifted copy of the rows, which goes token by token, gives the same bits."""
+    x, w, b, s, g, gen = conv_tensors(dtype, B, T, D, W, True, 0, 37)
+    lengths = conv_ragged(B, T, gen)
+    y, S, mag = conv(x, w, b, True, s, lengths)
+    last = torch.empty_like(s)
+    out = kb.kata_fwd_short_conv(x, w, b, silu=True, s_init=s, s_final=last, lengths=lengths)
+    within(out, y, conv_bound(y, mag, W, x.dtype, True), "out")
+    assert torch.equal(last.double(), S)
+    room = torch.empty(B, T, D + 8, device="cuda", dtype=x.dtype)
+    shifted = room[..., 1:1 + D]
+    shifted.copy_(x)
+    assert torch.equal(kb.kata_fwd_short_conv(shifted, w, b, silu=True, s_init=s, lengths=lengths), out)
+    assert torch.equal(kb.kata_bwd_short_conv(g, shifted, w, b, silu=True, lengths=lengths)[0], kb.kata_bwd_short_conv(g, x, w, b, silu=True, lengths=lengths)[0])
+    conv_backward(dtype, B, T, D, W, True, True, 0, True)
+
+
+def test_the_time_of_few_channels_does_not_grow_with_their_tiles():
+    """Sequences that fill an eighth of a tile, or less, are not worked on in tiles: with the same entries eight channels take no more
+    than four times what 1024 take (the walk 1.4 times; in tiles it was 13 and 6 times)."""
+    def us(f):
+        f()
+        a, z = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        best = 1e9
+        for _ in range(5):
+            torch.cuda.synchronize()
+            a.record()
+            for _ in range(10):
+                f()
+            z.record()
+            torch.cuda.synchronize()
+            best = min(best, a.elapsed_time(z) * 100)
+        return best
+
+    times = {}
+    for D in (8, 1024):
+        B, T = (1 << 24) // (128 * D), 128
+        x, w, b, _, g, _ = conv_tensors("bf16", B, T, D, 4, True, 0, 39)
+        out, dx, ws = torch.empty_like(x), torch.empty_like(x), kb.Workspace()
+        times[D] = (us(lambda: kb.kata_fwd_short_conv(x, w, b, silu=True, out=out)), us(lambda: kb.kata_bwd_short_conv(g, x, w, b, silu=True, dx=dx, workspace=ws)))
+    assert times[8][0] <= 4 * times[1024][0] and times[8][1] <= 4 * times[1024][1], times
