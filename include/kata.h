@@ -414,8 +414,8 @@ int kata_bwd_short_conv(const kata_short_conv_args* a, const kata_opts* opts);
  * Forms: bf16 with n in {64, 128}, d_v = 64 and more than 32 tokens (with s_final: 64) on the tensor cores, in chunks of 128
  * tokens: the weights inside a chunk, the values that enter the state which later chunks read, and that state as they read it are
  * rounded to bf16; s_final is exact to fp32.  Everything else goes token by token in fp32 (impl: KATA_IMPL_TENSOR / KATA_IMPL_SIMT
- * ask for one form; one row of q, k or v for all tokens, a token stride of 0, is the second's).  Few heads (sequences
- * of a padded batch counted as half full): the token axis is cut into segments, whose own states come first.  A NaN or infinity in a live token reaches, beside what follows it, the outputs of its own
+ * ask for one form; one row of q, k or v for all tokens, a token stride of 0, is the second's).  Few heads:
+ * the token axis is cut into segments, whose own states come first.  A NaN or infinity in a live token reaches, beside what follows it, the outputs of its own
  * chunk on the tensor cores (a weight of 0 times it).
  * Workspace: kata_workspace_bytes(KATA_FN_SSM_SCAN, B, H, T, n, d_v, 0, opts).
  * kata_decode_ssm_step: one token of every head, T = 1 (t-strides ignored, lengths null), s_init = s_final = the state; no workspace.

@@ -162,11 +162,6 @@ bool ssm_tensor(const CallOpts& o, int n, int d, int T, bool final_state) {
   return o.impl == KATA_IMPL_TENSOR || T > (final_state ? 64 : 32);
 }
 
-// Heads that a plan counts with.  With lengths the longest sequence of a padded batch fills it, the others are taken to be half as long
-// on average; their segments behind the end return at once.  Measured, us, 4 x 16 heads, 3001 tokens with a final state, two segments (as
-// without lengths) / three (by this rule): lengths uniform up to 3001: n = 128 66 / 58, n = 64 48.5 / 44.8; all of them 3001: n = 128 69 / 93.
-int ssm_heads(int B, int H, bool ragged) { return ragged ? (int)((long long)H * (B + 1) / 2) : B * H; }
-
 // Slots of states in the scratch (see SsmPlan).
 int ssm_slots(const SsmPlan& plan, bool tensor, bool final_state) {
   const int more = tensor && final_state ? 1 : 0;
@@ -203,7 +198,7 @@ int ssm(const kata_ssm_args* a, const kata_opts* opts, bool step) {
   for (const void* p : {(const void*)a->A, (const void*)a->D, (const void*)a->dt_bias, (const void*)a->lengths})
     if ((reinterpret_cast<uintptr_t>(p) & 3u) != 0) return KATA_ERR_ALIGNMENT;
   if ((reinterpret_cast<uintptr_t>(a->s_init) & 15u) != 0 || (reinterpret_cast<uintptr_t>(a->s_final) & 15u) != 0) return KATA_ERR_ALIGNMENT;
-  const SsmPlan plan = step ? SsmPlan{1, 1} : ssm_plan(ssm_heads(a->B, a->H, a->lengths != nullptr), T, a->n, a->d_v, tensor, r.s_final != nullptr);
+  const SsmPlan plan = step ? SsmPlan{1, 1} : ssm_plan(a->B * a->H, T, a->n, a->d_v, tensor, r.s_final != nullptr);
   if (tensor && T > 1 && (r.q.s2 == 0 || r.k.s2 == 0 || r.v.s2 == 0)) {      // (one row for all tokens has no tensor map)
     if (o.impl == KATA_IMPL_TENSOR) return KATA_ERR_UNSUPPORTED_SHAPE;
     tensor = false;
@@ -229,14 +224,13 @@ size_t mixer_workspace_bytes(int fn, int B, int H, int T, int d_k, int d_v, cons
   if (fn == KATA_FN_BWD_SHORT_CONV)
     return d_k >= 2 && d_k <= 4 && T <= kMaxTokens && H <= (1 << 24) && (double)B * T * H <= 1e11 ? align_up(short_conv_bwd_workspace_elems(B, T, H, d_k) * sizeof(float)) : 0;
   if (ssm_shape(B, H, T, d_k, d_v) != KATA_OK) return 0;
-  // (what a call with or without a final state, with or without lengths takes)
+  // (what a call with or without a final state takes)
   int slots = 0;
-  for (const bool last : {false, true})
-    for (const bool ragged : {false, true}) {
-      const bool tensor = ssm_tensor(o, d_k, d_v, T, last);
-      const int n = ssm_slots(ssm_plan(ssm_heads(B, H, ragged), T, d_k, d_v, tensor, last), tensor, last);
-      if (n > slots) slots = n;
-    }
+  for (const bool last : {false, true}) {
+    const bool tensor = ssm_tensor(o, d_k, d_v, T, last);
+    const int n = ssm_slots(ssm_plan(B * H, T, d_k, d_v, tensor, last), tensor, last);
+    if (n > slots) slots = n;
+  }
   return align_up(ssm_workspace_bytes(B * H, d_k, d_v, slots));
 }
 

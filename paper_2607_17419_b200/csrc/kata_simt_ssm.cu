@@ -216,6 +216,9 @@ template <typename T> void by_rows(const Ssm& a, const SsmPlan& plan, float* ws,
 // tensor cores, take the pass of the states too.  The smallest sum wins; more CTAs than eight per SM never did.  Measured, us with one
 // segment / two / this rule's: fp32, n = d_v = 64, 16 heads x 1000 tokens: 142 / 118 / 29; bf16, n = d_v = 16, 16 heads x 16384: 1320 /
 // 1035 / 58; fp32, n = d_v = 64, 128 heads x 2000 (the rule stays with one): 281 / 350 / 281.
+// The sequences of a padded batch count as if they filled it: their lengths are on the device.  (Counted as half full on average, with a
+// final state, us with lengths uniform / all full / one long among short, against this: 4 x 16 heads x 3001, n = 128: 54 to 61 / 86 / 46
+// against 62 / 63 / 61; 2 x 16 heads x 3001, n = 64: 30 to 43 / 42 / 28 against 30 / 30 / 30.)
 SsmPlan ssm_plan(int BH, int T, int n, int d, bool tensor, bool final_state) {
   const int tile = tensor ? 128 : 32, tiles = (T + tile - 1) / tile;
   const double out_us = tensor ? 1.85 : 2.0 + 0.039 * n, state_us = tensor ? 0.75 : 0.6 * out_us;

@@ -184,3 +184,15 @@ def test_the_time_of_few_channels_does_not_grow_with_their_tiles():
         out, dx, ws = torch.empty_like(x), torch.empty_like(x), kb.Workspace()
         times[D] = (us(lambda: kb.kata_fwd_short_conv(x, w, b, silu=True, out=out)), us(lambda: kb.kata_bwd_short_conv(g, x, w, b, silu=True, dx=dx, workspace=ws)))
     assert times[8][0] <= 4 * times[1024][0] and times[8][1] <= 4 * times[1024][1], times
+
+
+@pytest.mark.parametrize("B,H,T,n,dtype", [(2, 16, 3001, 64, "bf16"), (4, 16, 3001, 128, "bf16"), (3, 4, 2000, 32, "f32")])
+def test_a_full_batch_with_lengths_is_the_batch_without(B, H, T, n, dtype):
+    """The token axis is cut by the sizes alone: lengths that fill the batch change neither the segments nor a bit."""
+    q, k, v, dt, A, D, bias, init, _ = tensors(dtype, B, H, 1, T, n, 64, 41)
+    full = torch.full((B,), T, dtype=torch.int32, device="cuda")
+    for state in (False, True):
+        a, b = (torch.empty_like(init), torch.empty_like(init)) if state else (None, None)
+        with_lengths = kb.kata_fwd_ssm_scan(q, k, v, dt, A, D, bias, dt_softplus=True, s_init=init, s_final=a, lengths=full)
+        assert torch.equal(with_lengths, kb.kata_fwd_ssm_scan(q, k, v, dt, A, D, bias, dt_softplus=True, s_init=init, s_final=b))
+        assert a is None or torch.equal(a, b)
