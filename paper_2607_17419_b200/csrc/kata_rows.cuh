@@ -23,7 +23,6 @@ template <typename T, int N> struct Entries {
   typedef typename RawBytes<sizeof(T) * N>::type Raw;
   Raw raw;
   __device__ __forceinline__ void load(const void* p) { raw = *reinterpret_cast<const Raw*>(p); }
-  __device__ __forceinline__ void load_streaming(const void* p) { raw = __ldcs(reinterpret_cast<const Raw*>(p)); }
   __device__ __forceinline__ void store(void* p) const { *reinterpret_cast<Raw*>(p) = raw; }
   __device__ __forceinline__ void zero() { raw = Raw{}; }
   // (bf16 two at a time: an entry alone is converted on the pipe of the transcendental functions, an eighth as fast)

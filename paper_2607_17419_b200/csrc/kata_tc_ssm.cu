@@ -63,7 +63,7 @@ template <int N, int STATE> struct Shape {         // STATE: terms of the scaled
   static constexpr int HALVES = N / 64;                                        // 64-column halves of a q or k tile
   static constexpr uint32_t K_OFF = STATE ? 0 : HALVES * HALF, V_OFF = K_OFF + HALVES * HALF;
   static constexpr uint32_t STAGE = V_OFF + HALF;
-  static constexpr int NST = STATE ? (N == 64 ? 3 : 2) : (N == 64 ? 3 : 2);
+  static constexpr int NST = N == 64 ? 3 : 2;
   static constexpr int TERMS = STATE ? STATE : 1;
   static constexpr int XB = !STATE && N == 128 ? 1 : 2;                        // buffers of scaled V
   static constexpr uint32_t OFF_X = NST * STAGE;
@@ -133,20 +133,6 @@ __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
-}
-// Two fp32 operations in one instruction.
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-  float2 c;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(*reinterpret_cast<unsigned long long*>(&c))
-      : "l"(*reinterpret_cast<const unsigned long long*>(&a)), "l"(*reinterpret_cast<const unsigned long long*>(&b)));
-  return c;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(*reinterpret_cast<unsigned long long*>(&d))
-      : "l"(*reinterpret_cast<const unsigned long long*>(&a)), "l"(*reinterpret_cast<const unsigned long long*>(&b)),
-        "l"(*reinterpret_cast<const unsigned long long*>(&c)));
-  return d;
 }
 __device__ __forceinline__ float2 f2(uint32_t lo, uint32_t hi) { return make_float2(__uint_as_float(lo), __uint_as_float(hi)); }
 __device__ __forceinline__ float2 unpack(uint32_t x) { return f2(x << 16, x & 0xffff0000u); }
@@ -274,11 +260,11 @@ __device__ __forceinline__ void scaled_terms(const uint4& x, float w, uint4 (&ou
   uint32_t o[TERMS][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    float2 p = mul2(unpack(in[i]), make_float2(w, w));
+    float2 p = mul_pair(unpack(in[i]), make_float2(w, w));
 #pragma unroll
     for (int m = 0; m < TERMS; ++m) {
       o[m][i] = pack_bf16(p.x, p.y);
-      if (m + 1 < TERMS) p = fma2(unpack(o[m][i]), make_float2(-1.f, -1.f), p);
+      if (m + 1 < TERMS) p = fma_pair(unpack(o[m][i]), make_float2(-1.f, -1.f), p);
     }
   }
 #pragma unroll
@@ -485,7 +471,7 @@ tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           tmem_wait_ld(x);
 #pragma unroll
           for (int c = 0; c < 16; c += 2) {
-            const float2 n = fma2(keep, f2(S[c], S[c + 1]), f2(x[c], x[c + 1]));
+            const float2 n = fma_pair(keep, f2(S[c], S[c + 1]), f2(x[c], x[c + 1]));
             S[c] = __float_as_uint(n.x);
             S[c + 1] = __float_as_uint(n.y);
           }
@@ -572,7 +558,7 @@ tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 #pragma unroll
             for (int c = 0; c < 32; c += 4) {
               const float4 cf = col[c / 4];
-              const float2 u = mul2(mul2(make_float2(cf.x, cf.y), ff), f2(y[c], y[c + 1])), v = mul2(mul2(make_float2(cf.z, cf.w), ff), f2(y[c + 2], y[c + 3]));
+              const float2 u = mul_pair(mul_pair(make_float2(cf.x, cf.y), ff), f2(y[c], y[c + 1])), v = mul_pair(mul_pair(make_float2(cf.z, cf.w), ff), f2(y[c + 2], y[c + 3]));
               pk[c / 2] = pack_bf16(u.x, u.y);
               pk[c / 2 + 1] = pack_bf16(v.x, v.y);
             }
@@ -649,7 +635,7 @@ tc_ssm_out_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           uint32_t o[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const float2 z = fma2(unpack(in[i]), sk, fma2(f, f2(r[2 * i], r[2 * i + 1]), f2(y[2 * i], y[2 * i + 1])));
+            const float2 z = fma_pair(unpack(in[i]), sk, fma_pair(f, f2(r[2 * i], r[2 * i + 1]), f2(y[2 * i], y[2 * i + 1])));
             o[i] = dead ? 0u : pack_bf16(z.x, z.y);
           }
           *reinterpret_cast<uint4*>(rows + lane * 64 + (((2 * p) ^ ((lane >> 1) & 3)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
@@ -804,7 +790,7 @@ tc_ssm_state_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
         tmem_ld32(tmem_addr(tb, q4 * 32, COL_SL + b * DV + hf * 32), x);
         tmem_wait_ld(x);
 #pragma unroll
-        for (int c = 0; c < 16; ++c) S[hf * 16 + c] = fma2(make_float2(total, total), S[hf * 16 + c], f2(x[2 * c], x[2 * c + 1]));
+        for (int c = 0; c < 16; ++c) S[hf * 16 + c] = fma_pair(make_float2(total, total), S[hf * 16 + c], f2(x[2 * c], x[2 * c + 1]));
       }
       tc_fence_before();
       mbar_arrive(bars + BAR_SL_EMPTY + b);
