@@ -339,6 +339,8 @@ int kata_chunk_state_scan_static(const void* q, const void* k, const void* v, vo
  * R_p turns the pairs (i, i + rotary_dim / 2) (interleaved: (2i, 2i + 1)) of the first rotary_dim entries by p inv_freq[i]
  * radians; the others are left.  The angle is formed as a fraction of a turn in 64-bit integers, exact to 2^-64 p turns, so far
  * positions lose nothing.  Outputs are usually [B,H,T,d], what the attention takes.
+ *   The sum of a row's squares is fp32: rows with entries of 2^60 and beyond may give zeros, squares below 2^-126 count as zero (which
+ *   eps > 0 makes harmless).
  *   d in {16, 32, 64, 128}; rotary_dim a multiple of 16 up to d (0: norm alone); rows 16-byte aligned (KATA_ERR_ALIGNMENT);
  *   H_q, H_k <= 32767, B * T <= 2^31 - 1024.
  *   inv_freq: HOST array of rotary_dim / 2 values, read before the call returns.
@@ -378,6 +380,7 @@ int kata_bwd_norm_rope(const kata_norm_rope_args* a, const kata_opts* opts);
  * kata_decode_short_conv: one token, T = 1 (t-strides ignored), s_init and s_final set.
  * kata_bwd_short_conv: dout (read) takes the place of out; writes dx and, where set, dweight [D][width] and dbias [D] (fp32,
  * overwritten, summed in a fixed order).  s_init and s_final must be null: the sequences start at their first token.
+ * Tokens behind a sequence's end take no part in the sums.
  * Large enough calls whose rows are whole aligned 16-byte units (pointers, strides and D) go through shared memory, others from one
  * token to the next in registers, two channels or one at a time: out and dx are the same sums in the same order.
  * Workspace: kata_workspace_bytes(KATA_FN_BWD_SHORT_CONV, B, D, T, width, 0, 0, opts) for the backward, else none.
@@ -411,12 +414,14 @@ int kata_bwd_short_conv(const kata_short_conv_args* a, const kata_opts* opts);
  * distance, and what overflows fp32 on the way is inf or NaN in the result.
  *   s_init, s_final: [B,H,n,d_v] contiguous fp32, 16-byte aligned, the state before the first and after the last token of each
  *   sequence (either may be null; s_final may be s_init).
- * Forms: bf16 with n in {64, 128}, d_v = 64 and more than 32 tokens (with s_final: 64) on the tensor cores, in chunks of 128
- * tokens: the weights inside a chunk, the values that enter the state which later chunks read, and that state as they read it are
- * rounded to bf16; s_final is exact to fp32.  Everything else goes token by token in fp32 (impl: KATA_IMPL_TENSOR / KATA_IMPL_SIMT
- * ask for one form; one row of q, k or v for all tokens, a token stride of 0, is the second's).  Few heads:
- * the token axis is cut into segments, whose own states come first.  A NaN or infinity in a live token reaches, beside what follows it, the outputs of its own
- * chunk on the tensor cores (a weight of 0 times it).
+ * Forms.  bf16 with n in {64, 128}, d_v = 64 and more than 32 tokens (with s_final: 64) goes through the tensor cores, in chunks of
+ *   128 tokens, everything else token by token in fp32.  impl: KATA_IMPL_TENSOR / KATA_IMPL_SIMT ask for one form.  One row of q, k or v
+ *   for all tokens (a token stride of 0) is the second's.  Few heads: the token axis is cut into segments, by the sizes and whatever the
+ *   lengths, and the segments' own states come first.
+ * Precision of the tensor-core form: the weights inside a chunk, the values that enter the state which later chunks read, and that state
+ *   as they read it are rounded to bf16.  s_final is exact to fp32.
+ * A NaN or infinity in a live token reaches, beside what follows it, the outputs of its own chunk of 128 on the tensor cores (a weight
+ *   of 0 times it).
  * Workspace: kata_workspace_bytes(KATA_FN_SSM_SCAN, B, H, T, n, d_v, 0, opts).
  * kata_decode_ssm_step: one token of every head, T = 1 (t-strides ignored, lengths null), s_init = s_final = the state; no workspace.
  */

@@ -4,9 +4,11 @@
 // HBM-bound: every row is read and written once (backward: two reads, one write).  A row is held by d / (16 bytes) neighbouring
 // lanes.  A lane has both sides of its pairs, as two pieces of 8 bytes, so nothing but the sums of a row crosses lanes.  The turn of
 // a pair depends on the token and not on the head: the lanes of a token form their sines once and walk the heads with them.
-// Arithmetic goes two entries at a time.  Bound by latency more than by bandwidth: 8 x 4096 tokens, 32 heads of 64 in bf16, forward
-// and backward 161 us for 671 MB (three blocks of the backward and four of the forward on an SM; two and three: 181; one head in
-// flight less each: 164).
+// Arithmetic goes two entries at a time.  8 x 4096 tokens, 32 heads of 64: forward 48.5 us in bf16 and 87 in fp32, 0.85 and 0.94 of the
+// copy bandwidth; backward 108 and 164 (floor 61.5 and 123), pairs of neighbours 88 and 147.  The backward is bound by the latency of
+// its loads, with three blocks on an SM: the 80 registers that leaves spill 48 bytes in bf16 (neighbours 20), since a thread carries
+// the sums and the walk of queries and of keys.  (Forward and backward in bf16, 671 MB, 161 us together; two blocks of the backward and
+// three of the forward: 181; one head in flight less each: 164.)
 // Angles: position times a 64-bit fraction of a turn, in wrapping integers: no rounding grows with the position.
 #include "kata_rows.cuh"
 

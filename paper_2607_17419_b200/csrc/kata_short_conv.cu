@@ -13,8 +13,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kAhead = 2;              // tokens per load step; the next step's are on their way meanwhile
 
-// 1 / (1 + e^-z).  bf16: the approximate exponential and reciprocal (2^-21 relative, the result is rounded to 2^-9; 0 for z below
-// -88, where e^-z is inf).
+// 1 / (1 + e^-z).  bf16: the approximate exponential and reciprocal (2^-21 relative near 0; for negative z the rounding of the exponent
+// comes to |z| 2^-24, 2^-17 at -88; the result is rounded to 2^-8; 0 for z below -88, where e^-z is inf).
 template <typename T> __device__ __forceinline__ float sigmoid_of(float z) {
   if (sizeof(T) == 4) return 1.f / (1.f + expf(-z));
   float e, r;
@@ -500,9 +500,11 @@ __global__ void __launch_bounds__(kThreads) short_conv_tile_kernel(const __grid_
 }
 
 // A block has one group of channels and every gridDim.y-th tile: the next tile is on its way while one is worked on, and the sums of
-// the weights stay in registers.  8 x 4096 x 1024, forward and backward: 93 us (floor 51), bound by instructions and their latency
-// (122 registers; three and four blocks on an SM: 97, 93).  Not kept: a run's last gradients from the next run through shared memory
-// instead of once more (96), the sigmoid's constants in scalar instructions (95).  part: [gridDim.y][W + 1][D], or null
+// the weights stay in registers.  8 x 4096 x 1024: 70.8 us (floor 30.8), with the forward 95.9 (51), bound by instructions and their latency
+// (122 registers).  Two of them are what keeps the rows behind the end zero and out of the sums; a loop of its own for the runs at the
+// end took 72.4 and, with lengths between 1 and 4096, 83 instead of 50 to 59.  Not kept, measured before that with the forward (94 then): three
+// and four blocks on an SM (97, 93), a run's last gradients from the next run through shared memory instead of once more (96), the
+// sigmoid's constants in scalar instructions (95).  part: [gridDim.y][W + 1][D], or null
 template <typename T, int W, bool SILU>
 __global__ void __launch_bounds__(kThreads, 2) short_conv_bwd_tile_kernel(const __grid_constant__ ShortConv a, int tiles, unsigned n_tiles, int shift, bool wide,
                                                                           float* __restrict__ part) {

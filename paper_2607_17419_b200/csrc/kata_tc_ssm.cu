@@ -17,15 +17,14 @@
 //
 // Warps.  Out (768 threads): 0 decays; 1 issues Q K^T and Q S, 2 the tile's state and the product with V; 3 TMA loads;
 // 4-7 state; 8-15 weights and 16-23 scaled V and epilogue, two warps per TMEM lane quadrant.  State (512): 0 loads, 1 issues, 2, 3 decays, 4-7
-// state, 8-15 scaled V.  A warp reaches the next wait of its job long before the
-// others are done with theirs, so a tile takes the longest job and not their sum.  The jobs' loops are written once each and kept short: sixteen warps in unlike code of some thousand instructions each waited for instructions most of
-// the time (8 x 16 heads x 4096 tokens 135 us).
-// Measured (n = 64): 8 x 16 heads x 4096 tokens 59 us (144 MB: 22 us at the copy bandwidth; 3500 cycles a tile); 16 heads x 131072, in
-// segments with the state kernel before: 293 us (88 us).  Bound by instructions: a tile takes 8400 of the warps', two thirds of the issue
+// state, 8-15 scaled V.  A warp reaches the next wait of its job long before the others are done with theirs, so a tile takes the longest
+// job and not their sum.  The jobs' loops are written once each and kept short: sixteen warps in unlike code of some thousand instructions
+// each waited for instructions most of the time (8 x 16 heads x 4096 tokens 135 us).
+// Measured (n = 64): 8 x 16 heads x 4096 tokens 59.9 us (144 MB: 22 us at the copy bandwidth; 3500 cycles a tile); 16 heads x 131072, in
+// segments with the state kernel before: 294 us (88 us).  Bound by instructions: a tile takes 8400 of the warps', two thirds of the issue
 // slots with six warps a scheduler; the tensor cores and the memory wait.  Not kept: results in two buffers with weights in columns of
-// their own (65 us), an issuing warp for each chain (66 us), scaling V in bf16 pairs (59 us).
-// All waits are bounded; a warp that has TMEM to read goes on only where all its
-// lanes saw the barrier.
+// their own (65 us), an issuing warp for each chain (66 us), scaling V in bf16 pairs (59 us, as then without).
+// All waits are bounded; a warp that has TMEM to read goes on only where all its lanes saw the barrier.
 #include <cuda.h>
 
 #include "kata_rows.cuh"
